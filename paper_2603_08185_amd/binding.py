@@ -20,7 +20,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libserq.so")
 FASTCALL_PATH = os.path.join(_HERE, "_fastcall.so")
 
-F32, F16, BF16, I4 = 0, 1, 2, 3
+F32, F16, BF16, I4, F8 = 0, 1, 2, 3, 4
 PATH_AUTO, PATH_SKINNY, PATH_MFMA = 0, 1, 2
 
 _DT = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
@@ -68,6 +68,10 @@ SIGNATURES = {
     "serq_fp6_pack_weights": (_i, [_vp, _i64, _i64, _vp, _vp]),
     "serq_fp6_pack_act": (_i, [_vp, _i64, _i64, _vp, _vp]),
     "serq_proto_gemm_i32": (_i, [_vp, _vp, _i, _i64, _i64, _i64, _vp, _i64, _vp]),
+    "serq_kv_append": (_i, [_vp, _i64, _i64, _i, _vp, _i64, _i64, _vp, _i64, _i64, _i, _vp, _vp, _i64, _i, _i, _vp, _vp, _vp,
+                            _vp, _i64, _i64, _vp]),
+    "serq_paged_attn": (_i, [_vp, _i64, _i64, _i, _i, _vp, _vp, _i, _i64, C.c_float, _i, _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
+    "serq_paged_attn_workspace_bytes": (_sz, [_i64, _i, _i, _i64, _i, _i, _i]),
     "serq_bench_mfma_peak": (_i, [_vp, _i, _i, _vp, _vp]),
     "serq_bench_mfma_fp4_peak": (_i, [_vp, _i, _i, _vp, _vp]),
     "serq_bench_read": (_i, [_vp, _sz, _i, _vp, _vp]),
@@ -80,6 +84,8 @@ _fast_error = None      # why there is none
 # the entry points it calls, in the order of its bind()
 _FAST = ["serq_quantize_act", "serq_swiglu_quantize_act", "serq_mx_quantize_act", "serq_mx_swiglu_quantize_act",
          "serq_quantize_act_asym", "serq_linear", "serq_mx_linear", "serq_g128_linear"]
+# ... and in that of its bind_kv()
+_FAST_KV = ["serq_kv_append", "serq_paged_attn"]
 
 
 class SerqError(RuntimeError):
@@ -118,6 +124,7 @@ def _load_fastcall(L: C.CDLL) -> None:
         _fast_error = e
         return
     mod.bind(*(C.cast(getattr(L, name), C.c_void_p).value for name in _FAST))
+    mod.bind_kv(*(C.cast(getattr(L, name), C.c_void_p).value for name in _FAST_KV))
     _fast = mod
 
 
@@ -629,3 +636,136 @@ def proto_gemm_i32(X: torch.Tensor, W: torch.Tensor, fp6: bool, M: int, N: int, 
     _check("serq_proto_gemm_i32", lib().serq_proto_gemm_i32(_ptr(X), _ptr(W), 1 if fp6 else 0, M, N, K, _ptr(acc),
                                                             acc.stride(0) if M > 0 else N, _stream()))
     return acc
+
+
+# ---- the paged cache of keys and values, and attention over it ----------------------------------------------------
+class _KvCache(C.Structure):
+    """serq_kv_cache (include/serq_kv.h)."""
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp),
+                ("k_page", _i64), ("k_token", _i64), ("k_head", _i64), ("v_page", _i64), ("v_token", _i64), ("v_head", _i64),
+                ("pages", _i64), ("page_size", C.c_int32), ("heads", C.c_int32), ("dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class _KvBatch(C.Structure):
+    """serq_kv_batch (include/serq_kv.h)."""
+    _fields_ = [("cu_q", _vp), ("kv_len", _vp), ("table", _vp), ("table_ld", _i64), ("tokens", _i64),
+                ("table_width", C.c_int32), ("seqs", C.c_int32)]
+
+
+def _heads(T: torch.Tensor, what: str, dim: Optional[int] = None):
+    if not T.is_cuda:
+        raise ValueError(f"{what} must live in device memory")
+    if T.dim() != 3 or (T.stride(2) != 1 and T.numel() > 0) or (dim is not None and T.shape[2] != dim):
+        raise ValueError(f"{what} must be [tokens, heads, dim] with unit inner stride")
+
+
+def _kv_structs(K, V, table, cu_q, kv_len, tokens, dtype, k_scale, v_scale):
+    for t, what in ((K, "K"), (V, "V")):
+        if not t.is_cuda:
+            raise ValueError(f"{what} must live in device memory")
+        if t.dim() != 4 or (t.stride(3) != 1 and t.numel() > 0):
+            raise ValueError(f"{what} must be [pages, page_size, heads, dim] with unit inner stride")
+    if K.shape != V.shape or K.dtype != V.dtype:
+        raise ValueError("K and V must agree in shape and dtype")
+    for t, what, nd in ((table, "table", 2), (cu_q, "cu_q", 1), (kv_len, "kv_len", 1)):
+        if not t.is_cuda or t.dtype != torch.int32 or t.dim() != nd or (t.numel() > 0 and t.stride(-1) != 1):
+            raise ValueError(f"{what} must be int32 in device memory, {nd}-dimensional, with unit inner stride")
+    B = kv_len.shape[0]
+    if cu_q.shape[0] != B + 1 or table.shape[0] != B:
+        raise ValueError("cu_q has one entry more than there are sequences, table one row a sequence")
+    fp8 = K.dtype == torch.float8_e4m3fn
+    if not fp8 and K.dtype != dtype:
+        raise ValueError("the cache has the dtype of q, or float8_e4m3fn")
+    for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+        if t is not None and (not t.is_cuda or t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != K.shape[2] or not t.is_contiguous()):
+            raise ValueError(f"{what} must be fp32 [heads] in device memory")
+    c = _KvCache(_ptr(K), _ptr(V), _ptr(k_scale), _ptr(v_scale), K.stride(0), K.stride(1), K.stride(2), V.stride(0), V.stride(1),
+                 V.stride(2), K.shape[0], K.shape[1], K.shape[2], K.shape[3], F8 if fp8 else _DT[dtype])
+    b = _KvBatch(_ptr(cu_q), _ptr(kv_len), _ptr(table), max(table.stride(0), table.shape[1]) if B <= 1 else table.stride(0), tokens,
+                 table.shape[1], B)
+    return c, b
+
+
+def kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor,
+              cu_q: torch.Tensor, kv_len: torch.Tensor, cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
+              interleaved: bool = False, positions: Optional[torch.Tensor] = None, k_scale: Optional[torch.Tensor] = None,
+              v_scale: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """serq_kv_append: rotates q and k (tables cos, sin [positions, rotated channels / 2] fp32; None: no rotation), puts k and v into
+    the paged cache K, V [pages, page_size, heads, dim]; returns the rotated q (q None: keys and values only)."""
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    rc = (_fast or _native()).kv_append(q, k, v, K, V, table, cu_q, kv_len, cos, sin, 1 if interleaved else 0, positions, k_scale, v_scale,
+                                        q_out)
+    if rc == 0:
+        return q_out
+    if rc is not None:
+        raise SerqError("serq_kv_append", rc)
+    D = K.shape[-1]
+    for t, what in ((k, "k"), (v, "v"), (q, "q"), (q_out, "q_out")):
+        if t is not None:
+            _heads(t, what, D)
+            if t.shape[0] != k.shape[0] or t.dtype != k.dtype:
+                raise ValueError("q, k, v and q_out must agree in tokens and dtype")
+    if k.shape[1] != K.shape[2] or v.shape[1] != K.shape[2] or (q is not None and q_out.shape != q.shape):
+        raise ValueError("k and v must have the cache's heads, q_out q's")
+    rot = rows = 0
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin come together")
+    if cos is not None:
+        for t, what in ((cos, "cos"), (sin, "sin")):
+            if not t.is_cuda or t.dtype != torch.float32 or t.dim() != 2 or not t.is_contiguous() or t.shape != cos.shape:
+                raise ValueError(f"{what} must be fp32 [positions, rotated channels / 2] in device memory")
+        rows, rot = cos.shape[0], 2 * cos.shape[1]
+    if positions is not None and (not positions.is_cuda or positions.dtype != torch.int32 or positions.dim() != 1
+                                  or positions.shape[0] < k.shape[0] or (positions.numel() > 1 and positions.stride(0) != 1)):
+        raise ValueError("positions must be int32 [tokens] in device memory")
+    c, b = _kv_structs(K, V, table, cu_q, kv_len, k.shape[0], k.dtype, k_scale, v_scale)
+    rc = lib().serq_kv_append(_ptr(q), q.stride(0) if q is not None else 0, q.stride(1) if q is not None else 0,
+                              q.shape[1] if q is not None else 0, _ptr(k), k.stride(0), k.stride(1), _ptr(v), v.stride(0), v.stride(1),
+                              _DT[k.dtype], _ptr(cos), _ptr(sin), rows, rot, 1 if interleaved else 0, _ptr(positions), C.addressof(c),
+                              C.addressof(b), _ptr(q_out), q_out.stride(0) if q is not None else 0,
+                              q_out.stride(1) if q is not None else 0, _stream())
+    _check("serq_kv_append", rc)
+    return q_out
+
+
+def paged_attention_workspace(tokens: int, seqs: int, max_q: int, max_kv: int, q_heads: int, kv_heads: int, dim: int, device) -> torch.Tensor:
+    """A zeroed workspace for paged_attention (slices of a long cache)."""
+    n = lib().serq_paged_attn_workspace_bytes(tokens, seqs, max_q, max_kv, q_heads, kv_heads, dim)
+    if n == 0:
+        raise SerqError("serq_paged_attn_workspace_bytes", -3)
+    ws = torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+    _check("serq_workspace_init", lib().serq_workspace_init(_ptr(ws), ws.numel(), _stream()))
+    return ws
+
+
+def paged_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor,
+                    max_q: int, max_kv: int, scale: Optional[float] = None, window: int = 0, k_scale: Optional[torch.Tensor] = None,
+                    v_scale: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                    ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """serq_paged_attn: softmax(scale q K^T) V over the cached positions up to each new token's own (scale: 1 / sqrt(dim) by default;
+    window > 0: the last `window` of them); lse [tokens, q_heads] fp32 takes the logarithm of the softmax' sum."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if scale is None:
+        scale = q.shape[-1] ** -0.5
+    rc = (_fast or _native()).paged_attention(q, K, V, table, cu_q, kv_len, max_q, max_kv, scale, window, k_scale, v_scale, out, lse, ws)
+    if rc == 0:
+        return out
+    if rc is not None:
+        raise SerqError("serq_paged_attn", rc)
+    D = K.shape[-1]
+    for t, what in ((q, "q"), (out, "out")):
+        _heads(t, what, D)
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must agree with q in shape and dtype")
+    if lse is not None and (not lse.is_cuda or lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()):
+        raise ValueError("lse must be fp32 [tokens, q_heads] in device memory")
+    if ws is not None and (not ws.is_cuda or ws.dtype != torch.uint8 or not ws.is_contiguous()):
+        raise ValueError("ws must be a uint8 buffer in device memory")
+    c, b = _kv_structs(K, V, table, cu_q, kv_len, q.shape[0], q.dtype, k_scale, v_scale)
+    rc = lib().serq_paged_attn(_ptr(q), q.stride(0), q.stride(1), q.shape[1], _DT[q.dtype], C.addressof(c), C.addressof(b), max_q, max_kv,
+                               scale, window, _ptr(out), out.stride(0), out.stride(1), _ptr(lse), _ptr(ws),
+                               0 if ws is None else ws.numel(), _stream())
+    _check("serq_paged_attn", rc)
+    return out

@@ -12,7 +12,10 @@
 #include <ATen/core/Tensor.h>
 #include <c10/hip/HIPStream.h>
 
+#include <algorithm>
+
 #include "../../include/serq.h"
+#include "../../include/serq_kv.h"
 
 namespace {
 
@@ -24,6 +27,8 @@ decltype(&serq_quantize_act_asym) f_quantize_act_asym;
 decltype(&serq_linear) f_linear;
 decltype(&serq_mx_linear) f_mx_linear;
 decltype(&serq_g128_linear) f_g128_linear;
+decltype(&serq_kv_append) f_kv_append;
+decltype(&serq_paged_attn) f_paged_attn;
 
 // Arguments of one call; `ok` falls once one of them is not the plain thing.
 struct Args {
@@ -234,12 +239,127 @@ PyObject* g128_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- the paged cache: here every tensor's type and sizes are checked, as the general way does -------------------------------------
+// [tokens, heads, dim] with unit inner stride, in device memory
+struct Heads { void* p; int dt; int64_t T, H, D, ld, ldh; };
+Heads heads(Args& x, int i) {
+  Heads h{};
+  const at::Tensor* t = x.ok ? x.tensor(i) : nullptr;
+  if (!t || !t->is_cuda() || t->dim() != 3 || (t->stride(2) != 1 && t->numel() > 0)) { x.ok = false; return h; }
+  h = {t->data_ptr(), x.dtype(*t), t->size(0), t->size(1), t->size(2), t->stride(0), t->stride(1)};
+  if (h.dt == SERQ_F32) x.ok = false;
+  return h;
+}
+const at::Tensor* typed(Args& x, int i, at::ScalarType type, int64_t dims) {
+  const at::Tensor* t = x.ok ? x.tensor(i) : nullptr;
+  if (!t || !t->is_cuda() || t->scalar_type() != type || t->dim() != dims || (t->numel() > 0 && t->stride(dims - 1) != 1)) {
+    x.ok = false;
+    return nullptr;
+  }
+  return t;
+}
+const float* scales(Args& x, int i, int64_t n) {
+  if (!x.ok || x.a[i] == Py_None) return nullptr;
+  const at::Tensor* t = typed(x, i, at::kFloat, 1);
+  if (!t || t->size(0) != n) { x.ok = false; return nullptr; }
+  return (const float*)t->data_ptr();
+}
+// K, V, table, cu_q, kv_len from argument i on; k_scale, v_scale from argument s on
+struct Cache { serq_kv_cache c; serq_kv_batch b; };
+Cache cache(Args& x, int i, int s, const Heads& q) {
+  Cache r{};
+  const at::Tensor *K = x.ok ? x.tensor(i) : nullptr, *V = x.ok ? x.tensor(i + 1) : nullptr;
+  const at::Tensor *tb = typed(x, i + 2, at::kInt, 2), *cu = typed(x, i + 3, at::kInt, 1), *len = typed(x, i + 4, at::kInt, 1);
+  if (!x.ok) return r;
+  const bool f8 = K->scalar_type() == at::kFloat8_e4m3fn;
+  const int64_t B = len->size(0);
+  if (!K->is_cuda() || !V->is_cuda() || K->dim() != 4 || V->dim() != 4 || K->sizes() != V->sizes() || K->scalar_type() != V->scalar_type() ||
+      (K->numel() > 0 && (K->stride(3) != 1 || V->stride(3) != 1)) || (!f8 && x.dtype(*K) != q.dt) || cu->size(0) != B + 1 ||
+      tb->size(0) != B || K->size(3) != q.D || B > 65536 || tb->size(1) > 0x7fffffff || K->size(1) > 65536 || K->size(2) > 65536 || q.D > 65536) {
+    x.ok = false;
+    return r;
+  }
+  r.c = {K->data_ptr(), V->data_ptr(), scales(x, s, K->size(2)), scales(x, s + 1, K->size(2)), K->stride(0), K->stride(1), K->stride(2),
+         V->stride(0), V->stride(1), V->stride(2), K->size(0), (int32_t)K->size(1), (int32_t)K->size(2), (int32_t)K->size(3),
+         f8 ? SERQ_F8 : q.dt};
+  r.b = {(const int32_t*)cu->data_ptr(), (const int32_t*)len->data_ptr(), (const int32_t*)tb->data_ptr(),
+         B <= 1 ? std::max(tb->stride(0), tb->size(1)) : tb->stride(0), q.T, (int32_t)tb->size(1), (int32_t)B};
+  return r;
+}
+bool same_rows(const Heads& a, const Heads& b) { return a.T == b.T && a.D == b.D && a.dt == b.dt; }
+
+// q, k, v, K, V, table, cu_q, kv_len, cos, sin, interleaved, positions, k_scale, v_scale, q_out
+PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(a, n, 15, [](Args& x) {
+    Heads q{}, qo{};
+    const Heads k = heads(x, 1), v = heads(x, 2);
+    if (x.a[0] != Py_None) {
+      q = heads(x, 0);
+      qo = heads(x, 14);
+      if (!same_rows(q, k) || !same_rows(qo, k) || q.H != qo.H || q.H > 65536) x.ok = false;
+    }
+    const Cache c = cache(x, 3, 12, k);
+    const float *cs = nullptr, *sn = nullptr;
+    int64_t rows = 0, rot = 0;
+    if (x.a[8] != Py_None) {
+      const at::Tensor *ct = typed(x, 8, at::kFloat, 2), *st = typed(x, 9, at::kFloat, 2);
+      if (x.ok && (!ct->is_contiguous() || !st->is_contiguous() || ct->sizes() != st->sizes() || ct->size(1) > 65536)) x.ok = false;
+      if (x.ok) {
+        cs = (const float*)ct->data_ptr();
+        sn = (const float*)st->data_ptr();
+        rows = ct->size(0);
+        rot = 2 * ct->size(1);
+      }
+    } else if (x.a[9] != Py_None) {
+      x.ok = false;
+    }
+    const int inter = x.integer32(10);
+    const int32_t* pos = nullptr;
+    if (x.a[11] != Py_None) {
+      const at::Tensor* t = typed(x, 11, at::kInt, 1);
+      if (t && t->size(0) < k.T) x.ok = false;
+      if (t) pos = (const int32_t*)t->data_ptr();
+    }
+    if (!same_rows(k, v) || k.H != c.c.heads || v.H != c.c.heads) x.ok = false;
+    return [=](void* st) {
+      return f_kv_append(q.p, q.ld, q.ldh, (int)q.H, k.p, k.ld, k.ldh, v.p, v.ld, v.ldh, k.dt, cs, sn, rows, (int)rot, inter, pos, &c.c, &c.b,
+                         qo.p, qo.ld, qo.ldh, st);
+    };
+  });
+}
+
+// q, K, V, table, cu_q, kv_len, max_q, max_kv, scale, window, k_scale, v_scale, out, lse, ws
+PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(a, n, 15, [](Args& x) {
+    const Heads q = heads(x, 0), o = heads(x, 12);
+    const Cache c = cache(x, 1, 10, q);
+    const int max_q = x.integer32(6), window = x.integer32(9);
+    const int64_t max_kv = x.integer(7);
+    float scale = 0.0f;
+    if (PyFloat_CheckExact(x.a[8])) scale = (float)PyFloat_AS_DOUBLE(x.a[8]);
+    else x.ok = false;
+    float* lse = nullptr;
+    if (x.a[13] != Py_None) {
+      const at::Tensor* t = typed(x, 13, at::kFloat, 2);
+      if (t && (!t->is_contiguous() || t->size(0) != q.T || t->size(1) != q.H)) x.ok = false;
+      if (t) lse = (float*)t->data_ptr();
+    }
+    Room w{};
+    if (x.a[14] != Py_None) {
+      const at::Tensor* t = x.ok ? x.tensor(14) : nullptr;
+      if (t && (!t->is_cuda() || t->scalar_type() != at::kByte || !t->is_contiguous())) x.ok = false;
+      if (t && x.ok) w = {t->data_ptr(), (size_t)t->numel()};
+    }
+    if (!same_rows(q, o) || q.H != o.H || q.H > 65536) x.ok = false;
+    return [=](void* st) {
+      return f_paged_attn(q.p, q.ld, q.ldh, (int)q.H, q.dt, &c.c, &c.b, max_q, max_kv, scale, window, o.p, o.ld, o.ldh, lse, w.p, w.n, st);
+    };
+  });
+}
+
 // the addresses of the entry points, in the order of the declarations above
-PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void** const slots[] = {(void**)&f_quantize_act, (void**)&f_swiglu_quantize_act, (void**)&f_mx_quantize_act,
-                          (void**)&f_mx_swiglu_quantize_act, (void**)&f_quantize_act_asym, (void**)&f_linear,
-                          (void**)&f_mx_linear, (void**)&f_g128_linear};
-  if (n != (Py_ssize_t)(sizeof(slots) / sizeof(slots[0]))) {
+PyObject* bind_slots(void** const* slots, Py_ssize_t count, PyObject* const* a, Py_ssize_t n) {
+  if (n != count) {
     PyErr_SetString(PyExc_TypeError, "one address per entry point expected");
     return nullptr;
   }
@@ -254,10 +374,22 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void** const slots[] = {(void**)&f_quantize_act, (void**)&f_swiglu_quantize_act, (void**)&f_mx_quantize_act,
+                          (void**)&f_mx_swiglu_quantize_act, (void**)&f_quantize_act_asym, (void**)&f_linear,
+                          (void**)&f_mx_linear, (void**)&f_g128_linear};
+  return bind_slots(slots, sizeof(slots) / sizeof(slots[0]), a, n);
+}
+PyObject* bind_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void** const slots[] = {(void**)&f_kv_append, (void**)&f_paged_attn};
+  return bind_slots(slots, sizeof(slots) / sizeof(slots[0]), a, n);
+}
+
 #define SERQ_FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SERQ_FAST(bind), SERQ_FAST(quantize_act), SERQ_FAST(swiglu_quantize_act), SERQ_FAST(mx_quantize_act),
                          SERQ_FAST(mx_swiglu_quantize_act), SERQ_FAST(quantize_act_asym), SERQ_FAST(linear),
-                         SERQ_FAST(mx_linear), SERQ_FAST(g128_linear), {nullptr, nullptr, 0, nullptr}};
+                         SERQ_FAST(mx_linear), SERQ_FAST(g128_linear), SERQ_FAST(bind_kv), SERQ_FAST(kv_append),
+                         SERQ_FAST(paged_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
