@@ -32,7 +32,7 @@ typedef struct serq_kv_cache {
   void*        v;
   const float* k_scale;           /* SERQ_F8: [heads] fp32 each, NULL = ones; else ignored */
   const float* v_scale;
-  int64_t      k_page, k_token, k_head;   /* strides in elements, multiples of 16 bytes */
+  int64_t      k_page, k_token, k_head;   /* strides in elements, multiples of 16 bytes; k_token, v_token up to 2^26 */
   int64_t      v_page, v_token, v_head;
   int64_t      pages;             /* page numbers in table are 0 .. pages-1 */
   int32_t      page_size;         /* a power of two, 16 .. 65536 */

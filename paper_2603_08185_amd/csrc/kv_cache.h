@@ -43,6 +43,7 @@ inline int kv_check(const serq_kv_cache* c, const serq_kv_batch* b, int dtype, K
     if (s < 0 || s > ((int64_t)1 << 40)) return SERQ_ESHAPE;
     if (s % unit) return SERQ_EALIGN;
   }
+  if (c->k_token > (1 << 26) || c->v_token > (1 << 26)) return SERQ_ESHAPE;    // (16 rows lie within 2^31 bytes)
   if (b->tokens > 0 && b->seqs > 0) {
     if (!b->cu_q || !b->kv_len) return SERQ_ENULL;
     if (b->table_width > 0 && !b->table) return SERQ_ENULL;

@@ -1,0 +1,382 @@
+// serq_paged_attn for sequences with few rows (a token or a few, times the query heads of a key head): the cache is read once, and
+// everything else is there to keep it coming.
+//
+// A workgroup takes 16 NB rows, a key head and a slice of the keys; each of its four waves takes every fourth tile of 16 TG keys and walks alone,
+// with a running maximum, sum and weighted values of its own; the four meet in LDS at the end, and the slices of a sequence in the
+// workspace, where the last one to arrive joins them.
+//   scores   S^T = K Q^T on the 16x16x32 matrix instruction: keys are its rows, fetched from memory in the layout of its operand (a lane has
+//            16 bytes of one key), queries its columns, so that a lane's results are 4 keys of one row.
+//   weights  exp2(s c - m c), c = scale log2 e: one fused multiply-add and one exponential.  m is raised only when a score exceeds it by more than
+//            2^kSlack times in weight; between two raises no lane needs another's maximum.
+//   values   O^T = V^T P^T: the lane's weights are the instruction's operand as they stand (8 keys: 4 of one group of 16, 4 of the next); V goes
+//            through LDS, which reads it back by columns.
+// Weights are rounded to the 16-bit type for the product; their sum takes them unrounded.
+#include "paged_attn.h"
+
+namespace serq {
+namespace {
+
+constexpr float kSlack = 6.0f;
+constexpr int kWaves = 4;
+
+template <bool F8, int D> struct Few {
+  static constexpr int ROWB = D * (F8 ? 1 : 2);               // bytes of a key in the cache
+  static constexpr int TG = ROWB == 256 ? 2 : 4;              // groups of 16 keys in a tile
+  static constexpr int KEYS = 16 * TG;
+  static constexpr int KL = ROWB / 64;                        // 16-byte loads of a lane for 16 keys
+  static constexpr int LPR = ROWB / 16, RPI = 64 / LPR;       // V: lanes of a row, rows of a load
+  static constexpr int STEPS = D / 32;
+};
+
+template <int DT>
+__device__ __forceinline__ v4f mfma(const u4& a, const u4& b, const v4f& c) {
+  if constexpr (DT == SERQ_BF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
+
+// rows of V in LDS: 16-byte pieces, their place turned by the row so that 8 rows' equal pieces lie in different banks
+template <int D>
+__device__ __forceinline__ int turned(int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); }
+
+__device__ __forceinline__ void put2(float* p, float a, float b) {
+  const uint64_t v = (uint64_t)__float_as_uint(a) | (uint64_t)__float_as_uint(b) << 32;
+  __hip_atomic_store((uint64_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ v2f get2(const float* p) {
+  const uint64_t v = __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return (v2f){__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
+}
+
+template <int DT, bool F8, int D, int NB>
+__global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
+  using S = Few<F8, D>;
+  constexpr int TG = S::TG, KEYS = S::KEYS, KL = S::KL, BM = 16 * NB, VL = TG * KL;
+  constexpr int VBYTES = KEYS * D * 2;
+  constexpr int OPITCH = D + 4;                               // floats of a row where the waves meet
+  constexpr int MEET = BM * OPITCH * 4;
+  constexpr int REGION = VBYTES > MEET ? VBYTES : MEET;
+  __shared__ __align__(16) char lds[kWaves * REGION];
+  __shared__ float stat[kWaves][BM][2];
+  __shared__ uint32_t last;
+
+  const int tid = threadIdx.x, l = tid & 63, w = uniform(tid >> 6);
+  const int n16 = l & 15, quad = l >> 4;
+  const int h = blockIdx.y, s = blockIdx.z, G = p.group;
+  const RowBlock k = row_block<BM>(p, blockIdx.x, l);
+  if (k.rows <= 0) return;
+  const int base = k.begin & ~15;
+  // (more keys than the slices were made for: the last one takes them)
+  const int ns = k.end > base ? min((k.end - base - 1) / p.slice_keys + 1, p.slices) : 1;
+  if (s >= ns) return;
+  const int k0 = base + s * p.slice_keys, k1 = s == ns - 1 ? k.end : k0 + p.slice_keys;
+
+  // the rows' queries, and the keys that each sees: lo <= j < hi
+  const int tok0 = uniform(p.c.cu[k.b]);
+  u4 q[NB][S::STEPS];
+  int lo[NB], hi[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int r = k.r0 + 16 * nb + n16;
+    const bool live = 16 * nb + n16 < k.rows;
+    const int i = r / G, g = r - i * G;
+    hi[nb] = live ? min(k.L - k.n + i + 1, k.end) : 0;
+    lo[nb] = p.window > 0 ? max(0, k.L - k.n + i - p.window + 1) : 0;
+    const char* src = p.q + (int64_t)(tok0 + i) * p.ldq + (int64_t)(h * G + g) * p.ldqh;
+#pragma unroll
+    for (int st = 0; st < S::STEPS; ++st) {
+      // channels of step st that quad has: where its loads of K put them
+      const int at = F8 ? 64 * (st / 2) + 16 * quad + 8 * (st & 1) : 32 * st + 8 * quad;
+      q[nb][st] = live ? *(const u4*)(src + 2 * at) : (u4){0, 0, 0, 0};
+    }
+  }
+  // keys that all rows see: no mask there
+  const int all_lo = p.window > 0 ? max(0, k.L - k.n + (k.r0 + k.rows - 1) / G - p.window + 1) : 0;
+  const int all_hi = min(k.L - k.n + k.r0 / G + 1, k.end);
+  const float ks = p.c.k_scale ? p.c.k_scale[h] : 1.0f, vs = p.c.v_scale ? p.c.v_scale[h] : 1.0f;
+  const float c = p.scale * ks * kLog2e, slack = kSlack / c;
+
+  const int mask = (1 << p.c.page_shift) - 1;
+  const int32_t* table = p.c.table + k.b * p.c.table_ld;
+  const char* kbase = p.c.k + h * p.c.k_head;
+  const char* vbase = p.c.v + h * p.c.v_head;
+  const uint32_t klane = (uint32_t)(n16 * (int)p.c.k_token + quad * 16);
+  const uint32_t vlane = (uint32_t)((l / S::LPR) * (int)p.c.v_token + (l % S::LPR) * 16);
+
+  const int nt = k1 > k0 ? (k1 - k0 + KEYS - 1) / KEYS : 0;   // tiles of the slice
+  const int mine = nt > w ? (nt - w + kWaves - 1) / kWaves : 0;
+  // page numbers of the wave's next 64 / TG tiles, one group of 16 keys a lane (past the end: the last key's page)
+  int pages = 0;
+  auto look_up = [&](int t) {
+    const int key = min(k0 + (w + kWaves * (t + l / TG)) * KEYS + 16 * (l % TG), k.end - 1);
+    pages = min(max(table[key >> p.c.page_shift], 0), p.c.pages - 1);
+  };
+  u4 kr[TG][KL], vr[VL];
+  auto load_k = [&](int t) {
+    const int key0 = k0 + (w + kWaves * t) * KEYS;
+#pragma unroll
+    for (int a = 0; a < TG; ++a) {
+      const int pg = __builtin_amdgcn_readlane(pages, (t * TG + a) & 63);
+      const char* row = kbase + pg * p.c.k_page + ((key0 + 16 * a) & mask) * p.c.k_token;
+#pragma unroll
+      for (int i = 0; i < KL; ++i) kr[a][i] = *(const u4*)(row + klane + 64 * i);
+    }
+  };
+  auto load_v = [&](int t) {
+    const int key0 = k0 + (w + kWaves * t) * KEYS;
+#pragma unroll
+    for (int a = 0; a < TG; ++a) {
+      const int pg = __builtin_amdgcn_readlane(pages, (t * TG + a) & 63);
+      const char* row = vbase + pg * p.c.v_page + ((key0 + 16 * a) & mask) * p.c.v_token;
+#pragma unroll
+      for (int i = 0; i < KL; ++i) vr[a * KL + i] = *(const u4*)(row + i * S::RPI * p.c.v_token + vlane);
+    }
+  };
+
+  v4f o[NB][D / 16];
+  float m[NB], sum[NB];                                       // the reference times c; the lane's part of the sum of weights
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    m[nb] = -FLT_MAX;
+    sum[nb] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) o[nb][d] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  float ref[NB];                                              // the reference as a score
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) ref[nb] = -FLT_MAX;
+
+  char* my = lds + w * REGION;
+  const int vrow = l / S::LPR, vpiece = l % S::LPR;
+  // where a lane reads columns: keys 4 quad .. +3 of a group
+  const int crow = 4 * quad + n16 / 4;
+  const char* col = my + crow * D * 2 + ((n16 % 4) / 2) * 16 + (n16 & 1) * 8;
+  const int cturn = turned<D>(crow) << 4;
+
+  if (mine > 0) {
+    look_up(0);
+    load_k(0);
+    load_v(0);
+  }
+#pragma unroll 1
+  for (int t = 0; t < mine; ++t) {
+    const int key0 = k0 + (w + kWaves * t) * KEYS;
+    // scores
+    v4f sc[TG][NB];
+#pragma unroll
+    for (int a = 0; a < TG; ++a) {
+      u4 kk[S::STEPS];
+#pragma unroll
+      for (int i = 0; i < KL; ++i) {
+        if constexpr (F8) widen_e4m3<DT>(kr[a][i], kk[2 * i], kk[2 * i + 1]);
+        else kk[i] = kr[a][i];
+      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        sc[a][nb] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int st = 0; st < S::STEPS; ++st) sc[a][nb] = mfma<DT>(kk[st], q[nb][st], sc[a][nb]);
+      }
+    }
+    const bool more = t + 1 < mine;
+    if (more) {
+      if (((t + 1) * TG & 63) == 0) look_up(t + 1);
+      load_k(t + 1);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // V to LDS; rows that no row sees are zero there (a weight of zero does not make NaN zero)
+    const bool ends = key0 < k.begin || key0 + KEYS > k.end;
+#pragma unroll
+    for (int u = 0; u < VL; ++u) {
+      const int row = u * S::RPI + vrow;
+      u4 x = vr[u];
+      if (ends && (key0 + row < k.begin || key0 + row >= k.end)) x = (u4){0, 0, 0, 0};
+      char* at = my + row * D * 2;
+      if constexpr (F8) {
+        u4 a, b;
+        widen_e4m3<DT>(x, a, b);
+        at += ((2 * vpiece) ^ turned<D>(row)) << 4;
+        *(u4*)at = a;
+        *(u4*)(at + 16) = b;
+      } else {
+        *(u4*)(at + ((vpiece ^ turned<D>(row)) << 4)) = x;
+      }
+    }
+    if (more) load_v(t + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    // weights
+    if (key0 < all_lo || key0 + KEYS > all_hi) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int a = 0; a < TG; ++a)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = key0 + 16 * a + 4 * quad + e;
+            if (j < lo[nb] || j >= hi[nb]) sc[a][nb][e] = -INFINITY;
+          }
+    }
+    u4 pw[NB][TG / 2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float top = sc[0][nb][0];
+#pragma unroll
+      for (int a = 0; a < TG; ++a)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[a][nb][e]);
+      if (__ballot(top > ref[nb] + slack)) {
+        const float now = fmaxf(ref[nb], quads_reduce(top, [](float x, float y) { return fmaxf(x, y); }));
+        ref[nb] = now;
+        const float mc = fmaxf(now * c, -FLT_MAX), f = exp2_fast(m[nb] - mc);
+        m[nb] = mc;
+        sum[nb] *= f;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) o[nb][d] *= f;
+      }
+#pragma unroll
+      for (int a = 0; a < TG; ++a) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] = exp2_fast(__builtin_fmaf(sc[a][nb][e], c, -m[nb]));
+          sum[nb] += x[e];
+        }
+        pw[nb][a / 2][2 * (a & 1)] = pack16<DT>(x[0], x[1]);
+        pw[nb][a / 2][2 * (a & 1) + 1] = pack16<DT>(x[2], x[3]);
+      }
+    }
+    // values
+#pragma unroll
+    for (int st = 0; st < TG / 2; ++st)
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) {
+        const char* at = col + st * 32 * D * 2 + ((2 * d << 4) ^ cturn);
+        const u2 x = lds_column4(at), y = lds_column4(at + 16 * D * 2);
+        const u4 a = {x.x, x.y, y.x, y.y};
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) o[nb][d] = mfma<DT>(a, pw[nb][st], o[nb][d]);
+      }
+  }
+
+  // the waves meet
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const float all = quads_reduce(sum[nb], [](float x, float y) { return x + y; });
+    float* row = (float*)my + (16 * nb + n16) * OPITCH + 4 * quad;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) *(v4f*)(row + 16 * d) = o[nb][d];
+    if (quad == 0) {
+      stat[w][16 * nb + n16][0] = m[nb];
+      stat[w][16 * nb + n16][1] = all;
+    }
+  }
+  __syncthreads();
+  const int64_t head0 = (int64_t)h * G;
+  const bool sliced = ns > 1;
+  float* slot0 = p.part + ((int64_t)blockIdx.x * p.c.heads + h) * p.slices * (BM * (D + 2));
+  float* slot = slot0 + (int64_t)s * (BM * (D + 2));
+  for (int it = tid; it < k.rows * (D / 4); it += 256) {
+    const int r = it / (D / 4), d = 4 * (it % (D / 4));
+    float top = stat[0][r][0];
+#pragma unroll
+    for (int u = 1; u < kWaves; ++u) top = fmaxf(top, stat[u][r][0]);
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    float all = 0.0f;
+#pragma unroll
+    for (int u = 0; u < kWaves; ++u) {
+      const float f = exp2_fast(stat[u][r][0] - top);
+      all += f * stat[u][r][1];
+      acc += f * *(const v4f*)((const float*)(lds + u * REGION) + r * OPITCH + d);
+    }
+    if (sliced) {
+      put2(slot + r * D + d, acc[0], acc[1]);
+      put2(slot + r * D + d + 2, acc[2], acc[3]);
+      if (d == 0) put2(slot + BM * D + 2 * r, top, all);
+    } else {
+      const int i = (k.r0 + r) / G, g = k.r0 + r - i * G;
+      const float f = row_factor(all, vs);
+      char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (head0 + g) * p.ldoh;
+      *(u2*)(dst + 2 * d) = (u2){pack16<DT>(acc[0] * f, acc[1] * f), pack16<DT>(acc[2] * f, acc[3] * f)};
+      if (p.lse && d == 0) p.lse[(int64_t)(tok0 + i) * p.q_heads + head0 + g] = row_lse(top, all);
+    }
+  }
+  if (!sliced) return;
+
+  // the slices meet: a workgroup's stores are done (they go past the caches that other workgroups do not share) before it takes its
+  // ticket, and who draws the last one finds all of them
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0) last = __hip_atomic_fetch_add(p.tickets + (int64_t)blockIdx.x * p.c.heads + h, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (last != (uint32_t)(ns - 1)) return;
+  if (tid == 0) __hip_atomic_store(p.tickets + (int64_t)blockIdx.x * p.c.heads + h, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // weights of the slices, row by row (the regions of the waves are free)
+  float* weight = (float*)lds;                                // [rows][ns]
+  static_assert(BM * kMaxSlices * 4 <= kWaves * REGION, "the slices' weights");
+  for (int it = tid; it < k.rows * ns; it += 256) {
+    const int r = it / ns, u = it - r * ns;
+    weight[it] = get2(slot0 + (int64_t)u * (BM * (D + 2)) + BM * D + 2 * r)[0];
+  }
+  __syncthreads();
+  for (int r = w; r < k.rows; r += kWaves) {
+    float top = -FLT_MAX;
+    for (int u = l; u < ns; u += 64) top = fmaxf(top, weight[r * ns + u]);
+    top = wave_max(top);
+    float all = 0.0f;
+    for (int u = l; u < ns; u += 64) {
+      const float f = exp2_fast(weight[r * ns + u] - top);
+      weight[r * ns + u] = f;
+      all += f * get2(slot0 + (int64_t)u * (BM * (D + 2)) + BM * D + 2 * r)[1];
+    }
+    all = wave_reduce(all, [](float x, float y) { return x + y; });
+    if (l == 0) {
+      stat[0][r][0] = top;
+      stat[0][r][1] = all;
+    }
+  }
+  __syncthreads();
+  for (int it = tid; it < k.rows * (D / 2); it += 256) {
+    const int r = it / (D / 2), d = 2 * (it % (D / 2));
+    v2f acc = {0.0f, 0.0f};
+    const float* src = slot0 + r * D + d;
+    int u = 0;
+    for (; u + 8 <= ns; u += 8) {
+      v2f x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = get2(src + (int64_t)(u + e) * (BM * (D + 2)));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc += weight[r * ns + u + e] * x[e];
+    }
+    for (; u < ns; ++u) acc += weight[r * ns + u] * get2(src + (int64_t)u * (BM * (D + 2)));
+    const int i = (k.r0 + r) / G, g = k.r0 + r - i * G;
+    const float f = row_factor(stat[0][r][1], vs);
+    char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (head0 + g) * p.ldoh;
+    *(uint32_t*)(dst + 2 * d) = pack16<DT>(acc[0] * f, acc[1] * f);
+    if (p.lse && d == 0) p.lse[(int64_t)(tok0 + i) * p.q_heads + head0 + g] = row_lse(stat[0][r][0], stat[0][r][1]);
+  }
+}
+
+template <int DT, bool F8, int D>
+int launch(const AttnParams& p, int nb, int blocks, hipStream_t st) {
+  const dim3 grid((unsigned)blocks, (unsigned)p.c.heads, (unsigned)p.slices);
+  if (nb == 1) hipLaunchKernelGGL((paged_attn_few_kernel<DT, F8, D, 1>), grid, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((paged_attn_few_kernel<DT, F8, D, 2>), grid, dim3(256), 0, st, p);
+  return hipGetLastError() == hipSuccess ? SERQ_OK : SERQ_EHIP;
+}
+
+}  // namespace
+
+size_t paged_attn_few_slot_floats(int nb, int D) { return (size_t)16 * nb * (D + 2); }
+
+int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, int blocks, hipStream_t st) {
+  const bool bf = dtype == SERQ_BF16;
+  if (D == 128) {
+    if (bf) return f8 ? launch<SERQ_BF16, true, 128>(p, nb, blocks, st) : launch<SERQ_BF16, false, 128>(p, nb, blocks, st);
+    return f8 ? launch<SERQ_F16, true, 128>(p, nb, blocks, st) : launch<SERQ_F16, false, 128>(p, nb, blocks, st);
+  }
+  if (bf) return f8 ? launch<SERQ_BF16, true, 64>(p, nb, blocks, st) : launch<SERQ_BF16, false, 64>(p, nb, blocks, st);
+  return f8 ? launch<SERQ_F16, true, 64>(p, nb, blocks, st) : launch<SERQ_F16, false, 64>(p, nb, blocks, st);
+}
+
+}  // namespace serq

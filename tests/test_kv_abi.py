@@ -43,7 +43,7 @@ def test_cache_and_batch_are_checked(call):
     assert call(cache=False) == -1 and call(batch=False) == -1
     assert call(dt=0) == -2 and call(dt=3) == -2 and call(c=dict(dtype=1)) == -2 and call(c=dict(dtype=0)) == -2
     for bad in (dict(dim=96), dict(dim=256), dict(heads=0), dict(heads=1025), dict(pages=-1), dict(page_size=8), dict(page_size=24),
-                dict(page_size=131072), dict(k_page=-8), dict(v_head=-128)):
+                dict(page_size=131072), dict(k_page=-8), dict(v_head=-128), dict(k_token=(1 << 26) + 16)):
         assert call(c=bad) == -3, bad
     for bad in (dict(seqs=-1), dict(seqs=65537), dict(tokens=-1), dict(tokens=(1 << 24) + 1), dict(table_width=-1), dict(table_ld=2),
                 dict(table_width=1 << 30, table_ld=1 << 30)):
