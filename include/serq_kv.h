@@ -30,7 +30,7 @@ extern "C" {
 typedef struct serq_kv_cache {
   void*        k;                 /* element (page, row, head, d) at page*k_page + row*k_token + head*k_head + d */
   void*        v;
-  const float* k_scale;           /* SERQ_F8: [heads] fp32 each, NULL = ones; else ignored */
+  const float* k_scale;           /* SERQ_F8: [heads] fp32 each, positive, NULL = ones; else ignored */
   const float* v_scale;
   int64_t      k_page, k_token, k_head;   /* strides in elements, multiples of 16 bytes; k_token, v_token up to 2^26 */
   int64_t      v_page, v_token, v_head;
@@ -46,7 +46,7 @@ typedef struct serq_kv_batch {
   const int32_t* kv_len;          /* [seqs] */
   const int32_t* table;           /* [seqs, table_width], row stride table_ld */
   int64_t        table_ld;
-  int64_t        tokens;          /* rows of q, k, v and out: 0 .. 2^24 */
+  int64_t        tokens;          /* rows of q, k, v and out: 0 .. 2^22 */
   int32_t        table_width;
   int32_t        seqs;            /* 0 .. 65536 */
 } serq_kv_batch;
@@ -81,7 +81,8 @@ int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_heads,
  * holds, and pages that hold none of them are not read; their table entries may be anything.  Page numbers outside
  * 0 .. pages-1 are clamped, lengths past table_width * page_size cut (nothing is read out of bounds; the result is then
  * meaningless).
- *   q, out [tokens, q_heads, dim] in dtype (SERQ_F16 / SERQ_BF16), strides as above; q_heads a multiple of cache->heads.
+ *   q, out [tokens, q_heads, dim] in dtype (SERQ_F16 / SERQ_BF16), strides as above; q_heads a multiple of cache->heads.  tokens * q_heads is
+ *          at most 2^30, seqs * cache->heads 2^22.
  *   scale  positive and finite.
  *   max_q, max_kv  upper bounds of n_b and L_b, by which the kernel and the number of slices are chosen (host values; the results do not
  *          depend on them but for the order of fp32 sums).  More tokens or keys than that give SERQ_OK and wrong results, but

@@ -15,7 +15,6 @@ struct AttnParams {
   int64_t ldq, ldqh, ldo, ldoh;
   int q_heads, group, window;
   float scale;
-  int direct;             // every sequence fits one block of rows: block = sequence
   int rows_from, rows_to; // sequences with rows_from <= n G < rows_to are this kernel's
   int slices, slice_keys; // most slices of a sequence's keys, keys of one (a multiple of 256)
   uint32_t* tickets;      // [row blocks][key heads]: slices done, zero between calls
@@ -23,25 +22,26 @@ struct AttnParams {
   KvView c;
 };
 
-// Row blocks of BM rows: sequence b has the blocks from floor(cu[b] G / BM) + b on, up to where sequence b + 1's begin: at least as many as it
-// needs, in a place that no sum over the sequences before it is needed for.
 struct RowBlock {
   int b, r0, n, L;        // sequence, first row, new tokens, keys
   int rows;               // rows of the block (<= 0: none)
   int begin, end;         // keys that any of its rows sees: begin <= j < end
 };
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-template <int BM>
+// Block `block` of BM rows.  WHOLE: every sequence that is this kernel's fits one, and the block's number is the sequence's.  Else sequence b has the
+// blocks from floor(cu[b] G / BM) + b on, up to where sequence b + 1's begin: at least as many as it needs, in a place that takes no sum over the
+// sequences before it.
+template <int BM, bool WHOLE>
 __device__ __forceinline__ RowBlock row_block(const AttnParams& p, int block, int lane) {
   RowBlock k;
   const int G = p.group;
   k.rows = 0;
-  k.b = p.direct ? block : sequences_before(block, p.c.seqs, lane, [&](int i) { return p.c.cu[i + 1] * G / BM + i + 1; });
+  k.b = WHOLE ? block : sequences_before(block, p.c.seqs, lane, [&](int i) { return p.c.cu[i + 1] * G / BM + i + 1; });
   if (k.b >= p.c.seqs) return k;
   const int c0 = uniform(p.c.cu[k.b]), c1 = uniform(p.c.cu[k.b + 1]);
   k.n = c1 - c0;
   k.L = uniform(p.c.len[k.b]);
-  k.r0 = p.direct ? 0 : (block - (c0 * G / BM + k.b)) * BM;
+  k.r0 = WHOLE ? 0 : (block - (c0 * G / BM + k.b)) * BM;
   if (k.n <= 0 || k.n * G < p.rows_from || k.n * G >= p.rows_to || c0 < 0 || c1 > p.c.tokens) return k;
   k.rows = min(k.n * G - k.r0, BM);
   if (k.rows <= 0) return k;
@@ -63,6 +63,9 @@ __device__ __forceinline__ float quads_reduce(float v, const Op& op) {
   const auto b = __builtin_amdgcn_permlane32_swap(i, i, false, false);
   return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
+
+// by how much a score may exceed the reference before that is raised: 2^6 in weight
+__device__ __forceinline__ float score_slack(float c) { return fminf(6.0f / c, 1e30f); }
 
 // 16 E4M3 codes as 16-bit floats (exact in both types)
 template <int DT>
@@ -98,10 +101,97 @@ __device__ __forceinline__ float row_lse(float m, float l) {
   return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.693147180559945309f;
 }
 
-constexpr int kMaxSlices = 128;
+constexpr int kMaxSlices = 128;          // of the kernel for few rows
+constexpr int kMaxTileSlices = 32;       // of the kernel for many
+constexpr int kTileRows = 128;
 constexpr float kLog2e = 1.44269504088896341f;
 
+// ---- where the slices of a row block meet -------------------------------------------------------------------------------------
+// A slice leaves its weighted sums and the statistics (m, l) of its rows in a slot of the workspace: [rows][D] floats, then [rows][2].  The slots are
+// written and read past the caches that workgroups of different dies do not share (accesses at the device's scope).
+__device__ __forceinline__ void put2(float* p, float a, float b) {
+  const uint64_t v = (uint64_t)__float_as_uint(a) | (uint64_t)__float_as_uint(b) << 32;
+  __hip_atomic_store((uint64_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ v2f get2(const float* p) {
+  const uint64_t v = __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return (v2f){__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
+}
+// A workgroup's stores are done before it takes its ticket, and who draws the last one finds all of them; the count is left at zero.
+__device__ __forceinline__ bool last_to_arrive(uint32_t* ticket, int ns, int tid, uint32_t* shared) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0) {
+    const uint32_t n = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (n == (uint32_t)(ns - 1)) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *shared = n;
+  }
+  __syncthreads();
+  return *shared == (uint32_t)(ns - 1);
+}
+// The ns slots from slot0 on, joined and written out.  scratch: rows x (ns + 1) floats of LDS.
+template <int DT, int D, int BM, int THREADS>
+__device__ __forceinline__ void join_slices(const AttnParams& p, const RowBlock& k, int h, int ns, const float* slot0, float* scratch, int tok0,
+                                            float vs, int tid) {
+  constexpr int SLOT = BM * (D + 2);
+  const int l = tid & 63, w = uniform(tid >> 6);
+  float* weight = scratch + BM;                               // [rows][ns]: each slice's weight; scratch[row]: what the row is multiplied by
+  for (int r = w; r < k.rows; r += THREADS / 64) {
+    float m[(kMaxSlices + 63) / 64], n[(kMaxSlices + 63) / 64], top = -FLT_MAX;
+#pragma unroll
+    for (int e = 0; e < (kMaxSlices + 63) / 64; ++e) {
+      const int u = l + 64 * e;
+      m[e] = -FLT_MAX;
+      n[e] = 0.0f;
+      if (u < ns) {
+        const v2f x = get2(slot0 + (int64_t)u * SLOT + BM * D + 2 * r);
+        m[e] = x[0];
+        n[e] = x[1];
+      }
+      top = fmaxf(top, m[e]);
+    }
+    top = wave_max(top);
+    float all = 0.0f;
+#pragma unroll
+    for (int e = 0; e < (kMaxSlices + 63) / 64; ++e) {
+      const int u = l + 64 * e;
+      const float f = exp2_fast(m[e] - top);
+      if (u < ns) {
+        weight[r * ns + u] = f;
+        all += f * n[e];
+      }
+    }
+    all = wave_reduce(all, [](float x, float y) { return x + y; });
+    if (l == 0) {
+      scratch[r] = row_factor(all, vs);
+      const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
+      if (p.lse) p.lse[(int64_t)(tok0 + i) * p.q_heads + h * p.group + g] = row_lse(top, all);
+    }
+  }
+  __syncthreads();
+  for (int it = tid; it < k.rows * (D / 2); it += THREADS) {
+    const int r = it / (D / 2), d = 2 * (it % (D / 2));
+    v2f acc = {0.0f, 0.0f};
+    const float* src = slot0 + r * D + d;
+    int u = 0;
+    for (; u + 8 <= ns; u += 8) {                             // eight loads under way together
+      v2f x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = get2(src + (int64_t)(u + e) * SLOT);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc += weight[r * ns + u + e] * x[e];
+    }
+    for (; u < ns; ++u) acc += weight[r * ns + u] * get2(src + (int64_t)u * SLOT);
+    const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
+    const float f = scratch[r];
+    char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (int64_t)(h * p.group + g) * p.ldoh;
+    *(uint32_t*)(dst + 2 * d) = pack16<DT>(acc[0] * f, acc[1] * f);
+  }
+}
+
 size_t paged_attn_few_slot_floats(int nb, int D);
-int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, int blocks, hipStream_t st);
+int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, hipStream_t st);
+size_t paged_attn_tile_slot_floats(int D);
+int launch_paged_attn_tile(const AttnParams& p, int dtype, bool f8, int D, int blocks, hipStream_t st);
 
 }  // namespace serq

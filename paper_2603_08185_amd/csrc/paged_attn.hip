@@ -6,36 +6,57 @@ namespace {
 
 constexpr int kTickets = 4096;                                // words at the start of a workspace, whatever the call
 
+// Sequences with more rows than this go to the kernel for many.
+constexpr int kFewRows = 32;
+
+// (rows fit 31 bits, the threads of a grid 32)
+bool counts_ok(int64_t tokens, int64_t seqs, int q_heads, int heads) {
+  return tokens * q_heads <= (1 << 30) && seqs * heads <= (1 << 22);
+}
+
+// One kernel's share of a call.
 struct Plan {
-  int nb, blocks, slices, slice_keys, direct;
+  int blocks, slices, slice_keys;
   size_t bytes;
 };
 
-// keys: most that a row block can see
-Plan plan_few(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int heads, int group, int D) {
-  Plan k{};
+// Blocks of rows times key heads are the workgroups; while there are fewer than `want`, the keys (at most `keys` that a row block sees) are cut into
+// slices of at least `least` keys.
+Plan plan(int blocks, int heads, int64_t keys, int64_t want, int most, int least, size_t slot_floats) {
+  Plan k{blocks, 1, 0x7fffff00, 16};
+  const int64_t units = (int64_t)blocks * heads;
+  if (units <= 0 || units >= want || units > kTickets || keys <= least) return k;
+  int64_t n = (want + units - 1) / units;
+  if (n > most) n = most;
+  k.bytes = kTickets * 4 + (size_t)units * n * slot_floats * 4;
+  const int64_t each = ((keys + n - 1) / n + least - 1) / least * least;
+  k.slices = (int)((keys + each - 1) / each);
+  k.slice_keys = (int)each;
+  return k;
+}
+
+struct Plans {
+  bool few, many;         // which kernels have work
+  int nb;                 // few: blocks of 16 nb rows, one a sequence
+  Plan f, m;
+};
+
+Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int heads, int group, int D) {
+  Plans k{};
+  if (max_q > tokens) max_q = (int)tokens;
   const int64_t rows = (int64_t)max_q * group;
-  k.nb = rows <= 16 ? 1 : 2;
-  const int BM = 16 * k.nb;
-  k.direct = rows <= BM;
-  k.blocks = k.direct ? seqs : (int)(tokens * group / BM) + seqs;
-  const int64_t units = (int64_t)k.blocks * heads;
+  k.many = rows > kFewRows;
+  k.few = !k.many || (seqs > 1 && tokens < (int64_t)max_q * seqs);   // (a sequence alone, or all alike: none is short)
   int64_t keys = max_kv;
   if (window > 0 && keys > (int64_t)window + max_q) keys = (int64_t)window + max_q;
-  k.slices = 1;
-  k.slice_keys = 0x7fffff00;
-  k.bytes = 16;
-  const int64_t want = 4 * (int64_t)device_cu_count();
-  if (units > 0 && units < want && units <= kTickets && keys > 256) {
-    int64_t n = (want + units - 1) / units;
-    if (n > kMaxSlices) n = kMaxSlices;
-    k.bytes = kTickets * 4 + (size_t)units * n * paged_attn_few_slot_floats(k.nb, D) * 4;   // (the same with and without a window)
-    int64_t each = ((keys + n - 1) / n + 255) & ~(int64_t)255;
-    n = (keys + each - 1) / each;
-    if (n > 1) {
-      k.slices = (int)n;
-      k.slice_keys = (int)each;
-    }
+  const int64_t cus = device_cu_count();
+  if (k.few) {
+    k.nb = rows <= 16 ? 1 : 2;
+    k.f = plan(seqs, heads, keys, 4 * cus, kMaxSlices, 256, paged_attn_few_slot_floats(k.nb, D));
+  }
+  if (k.many) {
+    const int blocks = (int)(tokens * group / kTileRows) + seqs;
+    k.m = plan(blocks, heads, keys, 2 * cus, kMaxTileSlices, 512, paged_attn_tile_slot_floats(D));
   }
   return k;
 }
@@ -48,10 +69,11 @@ using namespace serq;
 extern "C" {
 
 size_t serq_paged_attn_workspace_bytes(int64_t tokens, int seqs, int max_q, int64_t max_kv, int q_heads, int kv_heads, int dim) {
-  if (tokens < 0 || tokens > (1 << 24) || seqs < 0 || seqs > 65536 || max_q < 0 || max_kv < 0 || kv_heads < 1 || kv_heads > 1024 ||
-      q_heads < 1 || q_heads > 65535 || q_heads % kv_heads || (dim != 64 && dim != 128) || tokens * (q_heads / kv_heads) > 0x7fffffff)
+  if (tokens < 0 || tokens > kKvTokens || seqs < 0 || seqs > 65536 || max_q < 0 || max_kv < 0 || kv_heads < 1 || kv_heads > 1024 ||
+      q_heads < 1 || q_heads > 65535 || q_heads % kv_heads || (dim != 64 && dim != 128) || !counts_ok(tokens, seqs, q_heads, kv_heads))
     return 0;
-  return plan_few(tokens, seqs, max_q, max_kv, 0, kv_heads, q_heads / kv_heads, dim).bytes;
+  const Plans k = plans(tokens, seqs, max_q, max_kv, 0, kv_heads, q_heads / kv_heads, dim);
+  return k.f.bytes > k.m.bytes ? k.f.bytes : k.m.bytes;       // (the two kernels of a call follow each other)
 }
 
 int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int dtype, const serq_kv_cache* cache,
@@ -63,7 +85,7 @@ int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int d
   if (rc != SERQ_OK) return rc;
   const int D = cache->dim;
   if (q_heads < 1 || q_heads > 65535 || q_heads % cache->heads || window < 0 || max_q < 0 || max_kv < 0) return SERQ_ESHAPE;
-  if (batch->tokens * (q_heads / cache->heads) > 0x7fffffff) return SERQ_ESHAPE;
+  if (!counts_ok(batch->tokens, batch->seqs, q_heads, cache->heads)) return SERQ_ESHAPE;
   if (!(scale > 0.0f) || !(scale <= FLT_MAX)) return SERQ_ESHAPE;
   if (batch->tokens == 0 || batch->seqs == 0) return SERQ_OK;
   if ((rc = kv_check_rows(q, ldq, ldqh, q_heads, D)) != SERQ_OK) return rc;
@@ -72,16 +94,29 @@ int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int d
   p.q = (const char*)q; p.out = (char*)out; p.lse = lse;
   p.ldq = 2 * ldq; p.ldqh = 2 * ldqh; p.ldo = 2 * ldo; p.ldoh = 2 * ldoh;
   p.q_heads = q_heads; p.group = q_heads / cache->heads; p.window = window; p.scale = scale;
-  if (max_q > batch->tokens) max_q = (int)batch->tokens;
-  const Plan k = plan_few(batch->tokens, batch->seqs, max_q, max_kv, window, cache->heads, p.group, D);
-  p.direct = k.direct;
-  p.rows_from = 0; p.rows_to = 0x7fffffff;
-  const bool sliced = k.slices > 1 && workspace && workspace_bytes >= k.bytes;
-  p.slices = sliced ? k.slices : 1;
-  p.slice_keys = sliced ? k.slice_keys : 0x7fffff00;
-  p.tickets = (uint32_t*)workspace;
-  p.part = (float*)workspace + kTickets;
-  return launch_paged_attn_few(p, dtype, cache->dtype == SERQ_F8, D, k.nb, k.blocks, (hipStream_t)stream);
+  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, window, cache->heads, p.group, D);
+  const auto place = [&](const Plan& n) {
+    const bool sliced = n.slices > 1 && workspace && workspace_bytes >= n.bytes;
+    p.slices = sliced ? n.slices : 1;
+    p.slice_keys = sliced ? n.slice_keys : 0x7fffff00;
+    p.tickets = (uint32_t*)workspace;
+    p.part = (float*)workspace + kTickets;
+  };
+  const bool f8 = cache->dtype == SERQ_F8;
+  if (k.many) {
+    p.rows_from = k.few ? kFewRows + 1 : 0;
+    p.rows_to = 0x7fffffff;
+    place(k.m);
+    rc = launch_paged_attn_tile(p, dtype, f8, D, k.m.blocks, (hipStream_t)stream);
+    if (rc != SERQ_OK) return rc;
+  }
+  if (k.few) {
+    p.rows_from = 0;
+    p.rows_to = k.many ? kFewRows + 1 : 0x7fffffff;
+    place(k.f);
+    rc = launch_paged_attn_few(p, dtype, f8, D, k.nb, (hipStream_t)stream);
+  }
+  return rc;
 }
 
 }  // extern "C"

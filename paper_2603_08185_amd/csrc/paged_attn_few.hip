@@ -7,7 +7,7 @@
 //   scores   S^T = K Q^T on the 16x16x32 matrix instruction: keys are its rows, fetched from memory in the layout of its operand (a lane has
 //            16 bytes of one key), queries its columns, so that a lane's results are 4 keys of one row.
 //   weights  exp2(s c - m c), c = scale log2 e: one fused multiply-add and one exponential.  m is raised only when a score exceeds it by more than
-//            2^kSlack times in weight; between two raises no lane needs another's maximum.
+//            2^6 in weight; between two raises no lane needs another's maximum.
 //   values   O^T = V^T P^T: the lane's weights are the instruction's operand as they stand (8 keys: 4 of one group of 16, 4 of the next); V goes
 //            through LDS, which reads it back by columns.
 // Weights are rounded to the 16-bit type for the product; their sum takes them unrounded.
@@ -16,7 +16,6 @@
 namespace serq {
 namespace {
 
-constexpr float kSlack = 6.0f;
 constexpr int kWaves = 4;
 
 template <bool F8, int D> struct Few {
@@ -40,15 +39,6 @@ __device__ __forceinline__ v4f mfma(const u4& a, const u4& b, const v4f& c) {
 template <int D>
 __device__ __forceinline__ int turned(int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); }
 
-__device__ __forceinline__ void put2(float* p, float a, float b) {
-  const uint64_t v = (uint64_t)__float_as_uint(a) | (uint64_t)__float_as_uint(b) << 32;
-  __hip_atomic_store((uint64_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ v2f get2(const float* p) {
-  const uint64_t v = __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return (v2f){__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
-}
-
 template <int DT, bool F8, int D, int NB>
 __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
   using S = Few<F8, D>;
@@ -64,7 +54,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
   const int tid = threadIdx.x, l = tid & 63, w = uniform(tid >> 6);
   const int n16 = l & 15, quad = l >> 4;
   const int h = blockIdx.y, s = blockIdx.z, G = p.group;
-  const RowBlock k = row_block<BM>(p, blockIdx.x, l);
+  const RowBlock k = row_block<BM, true>(p, blockIdx.x, l);
   if (k.rows <= 0) return;
   const int base = k.begin & ~15;
   // (more keys than the slices were made for: the last one takes them)
@@ -95,7 +85,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
   const int all_lo = p.window > 0 ? max(0, k.L - k.n + (k.r0 + k.rows - 1) / G - p.window + 1) : 0;
   const int all_hi = min(k.L - k.n + k.r0 / G + 1, k.end);
   const float ks = p.c.k_scale ? p.c.k_scale[h] : 1.0f, vs = p.c.v_scale ? p.c.v_scale[h] : 1.0f;
-  const float c = p.scale * ks * kLog2e, slack = kSlack / c;
+  const float c = p.scale * ks * kLog2e, slack = score_slack(c);
 
   const int mask = (1 << p.c.page_shift) - 1;
   const int32_t* table = p.c.table + k.b * p.c.table_ld;
@@ -273,7 +263,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
   }
   __syncthreads();
   const int64_t head0 = (int64_t)h * G;
-  const bool sliced = ns > 1;
+  const bool sliced = ns > 1;                                 // the slices of a sequence meet in the workspace
   float* slot0 = p.part + ((int64_t)blockIdx.x * p.c.heads + h) * p.slices * (BM * (D + 2));
   float* slot = slot0 + (int64_t)s * (BM * (D + 2));
   for (int it = tid; it < k.rows * (D / 4); it += 256) {
@@ -303,63 +293,14 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
   }
   if (!sliced) return;
 
-  // the slices meet: a workgroup's stores are done (they go past the caches that other workgroups do not share) before it takes its
-  // ticket, and who draws the last one finds all of them
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (tid == 0) last = __hip_atomic_fetch_add(p.tickets + (int64_t)blockIdx.x * p.c.heads + h, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  if (last != (uint32_t)(ns - 1)) return;
-  if (tid == 0) __hip_atomic_store(p.tickets + (int64_t)blockIdx.x * p.c.heads + h, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  // weights of the slices, row by row (the regions of the waves are free)
-  float* weight = (float*)lds;                                // [rows][ns]
-  static_assert(BM * kMaxSlices * 4 <= kWaves * REGION, "the slices' weights");
-  for (int it = tid; it < k.rows * ns; it += 256) {
-    const int r = it / ns, u = it - r * ns;
-    weight[it] = get2(slot0 + (int64_t)u * (BM * (D + 2)) + BM * D + 2 * r)[0];
-  }
-  __syncthreads();
-  for (int r = w; r < k.rows; r += kWaves) {
-    float top = -FLT_MAX;
-    for (int u = l; u < ns; u += 64) top = fmaxf(top, weight[r * ns + u]);
-    top = wave_max(top);
-    float all = 0.0f;
-    for (int u = l; u < ns; u += 64) {
-      const float f = exp2_fast(weight[r * ns + u] - top);
-      weight[r * ns + u] = f;
-      all += f * get2(slot0 + (int64_t)u * (BM * (D + 2)) + BM * D + 2 * r)[1];
-    }
-    all = wave_reduce(all, [](float x, float y) { return x + y; });
-    if (l == 0) {
-      stat[0][r][0] = top;
-      stat[0][r][1] = all;
-    }
-  }
-  __syncthreads();
-  for (int it = tid; it < k.rows * (D / 2); it += 256) {
-    const int r = it / (D / 2), d = 2 * (it % (D / 2));
-    v2f acc = {0.0f, 0.0f};
-    const float* src = slot0 + r * D + d;
-    int u = 0;
-    for (; u + 8 <= ns; u += 8) {
-      v2f x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = get2(src + (int64_t)(u + e) * (BM * (D + 2)));
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc += weight[r * ns + u + e] * x[e];
-    }
-    for (; u < ns; ++u) acc += weight[r * ns + u] * get2(src + (int64_t)u * (BM * (D + 2)));
-    const int i = (k.r0 + r) / G, g = k.r0 + r - i * G;
-    const float f = row_factor(stat[0][r][1], vs);
-    char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (head0 + g) * p.ldoh;
-    *(uint32_t*)(dst + 2 * d) = pack16<DT>(acc[0] * f, acc[1] * f);
-    if (p.lse && d == 0) p.lse[(int64_t)(tok0 + i) * p.q_heads + head0 + g] = row_lse(stat[0][r][0], stat[0][r][1]);
-  }
+  if (!last_to_arrive(p.tickets + (int64_t)blockIdx.x * p.c.heads + h, ns, tid, &last)) return;
+  static_assert(BM * (kMaxSlices + 1) * 4 <= kWaves * REGION, "the slices' weights");
+  join_slices<DT, D, BM, 256>(p, k, h, ns, slot0, (float*)lds, tok0, vs, tid);   // (the regions of the waves are free)
 }
 
 template <int DT, bool F8, int D>
-int launch(const AttnParams& p, int nb, int blocks, hipStream_t st) {
-  const dim3 grid((unsigned)blocks, (unsigned)p.c.heads, (unsigned)p.slices);
+int launch(const AttnParams& p, int nb, hipStream_t st) {
+  const dim3 grid((unsigned)p.c.seqs, (unsigned)p.c.heads, (unsigned)p.slices);
   if (nb == 1) hipLaunchKernelGGL((paged_attn_few_kernel<DT, F8, D, 1>), grid, dim3(256), 0, st, p);
   else hipLaunchKernelGGL((paged_attn_few_kernel<DT, F8, D, 2>), grid, dim3(256), 0, st, p);
   return hipGetLastError() == hipSuccess ? SERQ_OK : SERQ_EHIP;
@@ -369,14 +310,14 @@ int launch(const AttnParams& p, int nb, int blocks, hipStream_t st) {
 
 size_t paged_attn_few_slot_floats(int nb, int D) { return (size_t)16 * nb * (D + 2); }
 
-int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, int blocks, hipStream_t st) {
+int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, hipStream_t st) {
   const bool bf = dtype == SERQ_BF16;
   if (D == 128) {
-    if (bf) return f8 ? launch<SERQ_BF16, true, 128>(p, nb, blocks, st) : launch<SERQ_BF16, false, 128>(p, nb, blocks, st);
-    return f8 ? launch<SERQ_F16, true, 128>(p, nb, blocks, st) : launch<SERQ_F16, false, 128>(p, nb, blocks, st);
+    if (bf) return f8 ? launch<SERQ_BF16, true, 128>(p, nb, st) : launch<SERQ_BF16, false, 128>(p, nb, st);
+    return f8 ? launch<SERQ_F16, true, 128>(p, nb, st) : launch<SERQ_F16, false, 128>(p, nb, st);
   }
-  if (bf) return f8 ? launch<SERQ_BF16, true, 64>(p, nb, blocks, st) : launch<SERQ_BF16, false, 64>(p, nb, blocks, st);
-  return f8 ? launch<SERQ_F16, true, 64>(p, nb, blocks, st) : launch<SERQ_F16, false, 64>(p, nb, blocks, st);
+  if (bf) return f8 ? launch<SERQ_BF16, true, 64>(p, nb, st) : launch<SERQ_BF16, false, 64>(p, nb, st);
+  return f8 ? launch<SERQ_F16, true, 64>(p, nb, st) : launch<SERQ_F16, false, 64>(p, nb, st);
 }
 
 }  // namespace serq

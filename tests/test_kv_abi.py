@@ -45,7 +45,7 @@ def test_cache_and_batch_are_checked(call):
     for bad in (dict(dim=96), dict(dim=256), dict(heads=0), dict(heads=1025), dict(pages=-1), dict(page_size=8), dict(page_size=24),
                 dict(page_size=131072), dict(k_page=-8), dict(v_head=-128), dict(k_token=(1 << 26) + 16)):
         assert call(c=bad) == -3, bad
-    for bad in (dict(seqs=-1), dict(seqs=65537), dict(tokens=-1), dict(tokens=(1 << 24) + 1), dict(table_width=-1), dict(table_ld=2),
+    for bad in (dict(seqs=-1), dict(seqs=65537), dict(tokens=-1), dict(tokens=(1 << 22) + 1), dict(table_width=-1), dict(table_ld=2),
                 dict(table_width=1 << 30, table_ld=1 << 30)):
         assert call(b=bad) == -3, bad
     for bad in (dict(k_token=260), dict(v_page=4), dict(k=ODD), dict(v=OFF4), dict(dtype=4, k_token=264), dict(dtype=4, v_scale=ODD)):
@@ -72,7 +72,7 @@ def test_append_refuses():
 def test_attention_refuses():
     for bad in (dict(Hq=0), dict(Hq=7), dict(Hq=65536), dict(window=-1), dict(max_q=-1), dict(max_kv=-1), dict(scale=0.0), dict(scale=-1.0),
                 dict(scale=float("nan")), dict(scale=float("inf")), dict(ldqh=64), dict(ldo=-8), dict(ldoh=120),
-                dict(Hq=2048, ldqh=128, b=dict(tokens=1 << 24), c=dict(heads=1))):
+                dict(Hq=2048, b=dict(tokens=1 << 22)), dict(Hq=1024, b=dict(seqs=65536), c=dict(heads=128))):
         assert _attn(**bad) == -3, bad
     for bad in (dict(q=None), dict(o=None)):
         assert _attn(**bad) == -1, bad
