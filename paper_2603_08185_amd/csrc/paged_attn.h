@@ -18,7 +18,7 @@ struct AttnParams {
   int rows_from, rows_to; // sequences with rows_from <= n G < rows_to are this kernel's
   int slices, slice_keys; // most slices of a sequence's keys, keys of one (a multiple of 256)
   uint32_t* tickets;      // [row blocks][key heads]: slices done, zero between calls
-  float* part;            // [row blocks][key heads][slices]: rows x D sums, then rows x 2 statistics
+  float* part;            // [row blocks][key heads][slices]: the slots where slices meet
   KvView c;
 };
 
@@ -107,8 +107,9 @@ constexpr int kTileRows = 128;
 constexpr float kLog2e = 1.44269504088896341f;
 
 // ---- where the slices of a row block meet -------------------------------------------------------------------------------------
-// A slice leaves its weighted sums and the statistics (m, l) of its rows in a slot of the workspace: [rows][D] floats, then [rows][2].  The slots are
-// written and read past the caches that workgroups of different dies do not share (accesses at the device's scope).
+// A slice leaves its weighted sums and the statistics (m, l) of its rows in a slot of the workspace: rows x D floats in an order of the kernel's own,
+// then [rows][2].  The slots are written and read past the caches that workgroups of different dies do not share (accesses at the
+// device's scope).
 __device__ __forceinline__ void put2(float* p, float a, float b) {
   const uint64_t v = (uint64_t)__float_as_uint(a) | (uint64_t)__float_as_uint(b) << 32;
   __hip_atomic_store((uint64_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -129,66 +130,6 @@ __device__ __forceinline__ bool last_to_arrive(uint32_t* ticket, int ns, int tid
   __syncthreads();
   return *shared == (uint32_t)(ns - 1);
 }
-// The ns slots from slot0 on, joined and written out.  scratch: rows x (ns + 1) floats of LDS.
-template <int DT, int D, int BM, int THREADS>
-__device__ __forceinline__ void join_slices(const AttnParams& p, const RowBlock& k, int h, int ns, const float* slot0, float* scratch, int tok0,
-                                            float vs, int tid) {
-  constexpr int SLOT = BM * (D + 2);
-  const int l = tid & 63, w = uniform(tid >> 6);
-  float* weight = scratch + BM;                               // [rows][ns]: each slice's weight; scratch[row]: what the row is multiplied by
-  for (int r = w; r < k.rows; r += THREADS / 64) {
-    float m[(kMaxSlices + 63) / 64], n[(kMaxSlices + 63) / 64], top = -FLT_MAX;
-#pragma unroll
-    for (int e = 0; e < (kMaxSlices + 63) / 64; ++e) {
-      const int u = l + 64 * e;
-      m[e] = -FLT_MAX;
-      n[e] = 0.0f;
-      if (u < ns) {
-        const v2f x = get2(slot0 + (int64_t)u * SLOT + BM * D + 2 * r);
-        m[e] = x[0];
-        n[e] = x[1];
-      }
-      top = fmaxf(top, m[e]);
-    }
-    top = wave_max(top);
-    float all = 0.0f;
-#pragma unroll
-    for (int e = 0; e < (kMaxSlices + 63) / 64; ++e) {
-      const int u = l + 64 * e;
-      const float f = exp2_fast(m[e] - top);
-      if (u < ns) {
-        weight[r * ns + u] = f;
-        all += f * n[e];
-      }
-    }
-    all = wave_reduce(all, [](float x, float y) { return x + y; });
-    if (l == 0) {
-      scratch[r] = row_factor(all, vs);
-      const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
-      if (p.lse) p.lse[(int64_t)(tok0 + i) * p.q_heads + h * p.group + g] = row_lse(top, all);
-    }
-  }
-  __syncthreads();
-  for (int it = tid; it < k.rows * (D / 2); it += THREADS) {
-    const int r = it / (D / 2), d = 2 * (it % (D / 2));
-    v2f acc = {0.0f, 0.0f};
-    const float* src = slot0 + r * D + d;
-    int u = 0;
-    for (; u + 8 <= ns; u += 8) {                             // eight loads under way together
-      v2f x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = get2(src + (int64_t)(u + e) * SLOT);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc += weight[r * ns + u + e] * x[e];
-    }
-    for (; u < ns; ++u) acc += weight[r * ns + u] * get2(src + (int64_t)u * SLOT);
-    const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
-    const float f = scratch[r];
-    char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (int64_t)(h * p.group + g) * p.ldoh;
-    *(uint32_t*)(dst + 2 * d) = pack16<DT>(acc[0] * f, acc[1] * f);
-  }
-}
-
 size_t paged_attn_few_slot_floats(int nb, int D);
 int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, hipStream_t st);
 size_t paged_attn_tile_slot_floats(int D);

@@ -39,6 +39,66 @@ __device__ __forceinline__ v4f mfma(const u4& a, const u4& b, const v4f& c) {
 template <int D>
 __device__ __forceinline__ int turned(int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); }
 
+// The ns slots from slot0 on, joined and written out.  scratch: rows x (ns + 1) floats of LDS.
+template <int DT, int D, int BM, int THREADS>
+__device__ __forceinline__ void join_slices(const AttnParams& p, const RowBlock& k, int h, int ns, const float* slot0, float* scratch, int tok0,
+                                            float vs, int tid) {
+  constexpr int SLOT = BM * (D + 2);
+  const int l = tid & 63, w = uniform(tid >> 6);
+  float* weight = scratch + BM;                               // [rows][ns]: each slice's weight; scratch[row]: what the row is multiplied by
+  for (int r = w; r < k.rows; r += THREADS / 64) {
+    float m[(kMaxSlices + 63) / 64], n[(kMaxSlices + 63) / 64], top = -FLT_MAX;
+#pragma unroll
+    for (int e = 0; e < (kMaxSlices + 63) / 64; ++e) {
+      const int u = l + 64 * e;
+      m[e] = -FLT_MAX;
+      n[e] = 0.0f;
+      if (u < ns) {
+        const v2f x = get2(slot0 + (int64_t)u * SLOT + BM * D + 2 * r);
+        m[e] = x[0];
+        n[e] = x[1];
+      }
+      top = fmaxf(top, m[e]);
+    }
+    top = wave_max(top);
+    float all = 0.0f;
+#pragma unroll
+    for (int e = 0; e < (kMaxSlices + 63) / 64; ++e) {
+      const int u = l + 64 * e;
+      const float f = exp2_fast(m[e] - top);
+      if (u < ns) {
+        weight[r * ns + u] = f;
+        all += f * n[e];
+      }
+    }
+    all = wave_reduce(all, [](float x, float y) { return x + y; });
+    if (l == 0) {
+      scratch[r] = row_factor(all, vs);
+      const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
+      if (p.lse) p.lse[(int64_t)(tok0 + i) * p.q_heads + h * p.group + g] = row_lse(top, all);
+    }
+  }
+  __syncthreads();
+  for (int it = tid; it < k.rows * (D / 2); it += THREADS) {
+    const int r = it / (D / 2), d = 2 * (it % (D / 2));
+    v2f acc = {0.0f, 0.0f};
+    const float* src = slot0 + r * D + d;
+    int u = 0;
+    for (; u + 8 <= ns; u += 8) {                             // eight loads under way together
+      v2f x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = get2(src + (int64_t)(u + e) * SLOT);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc += weight[r * ns + u + e] * x[e];
+    }
+    for (; u < ns; ++u) acc += weight[r * ns + u] * get2(src + (int64_t)u * SLOT);
+    const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
+    const float f = scratch[r];
+    char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (int64_t)(h * p.group + g) * p.ldoh;
+    *(uint32_t*)(dst + 2 * d) = pack16<DT>(acc[0] * f, acc[1] * f);
+  }
+}
+
 template <int DT, bool F8, int D, int NB>
 __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
   using S = Few<F8, D>;

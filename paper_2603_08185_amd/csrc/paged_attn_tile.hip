@@ -223,40 +223,56 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(AttnParams 
 
   const uint32_t sbits = __float_as_uint(sum);
   const auto both = __builtin_amdgcn_permlane32_swap(sbits, sbits, false, false);
-  const float all = __uint_as_float(both[0]) + __uint_as_float(both[1]);
-  if (ns == 1) {
-    if (!live) return;
-    const float f = row_factor(all, vs);
-    char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (int64_t)(h * G + g) * p.ldoh;
+  float all = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+  if (ns > 1) {
+    // The slices meet in the workspace, register by register: pair j of thread t lies at [j][t], so that a wave's accesses are whole lines.  They
+    // are added in their order, whoever comes last.
+    constexpr int SLOT = BM * (D + 2);
+    float* slot0 = p.part + ((int64_t)block * p.c.heads + h) * p.slices * SLOT;
+    float* slot = slot0 + (int64_t)s * SLOT;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        *(u2*)(dst + 2 * (32 * d + 8 * e + 4 * half)) = (u2){pack16<DT>(o[d][4 * e] * f, o[d][4 * e + 1] * f),
-                                                             pack16<DT>(o[d][4 * e + 2] * f, o[d][4 * e + 3] * f)};
-    if (p.lse && half == 0) p.lse[(int64_t)(tok0 + i) * p.q_heads + h * G + g] = row_lse(m, all);
-    return;
-  }
-
-  // ---- the slices meet in the workspace
-  constexpr int SLOT = BM * (D + 2);
-  float* slot0 = p.part + ((int64_t)block * p.c.heads + h) * p.slices * SLOT;
-  float* slot = slot0 + (int64_t)s * SLOT;
-  if (live) {
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float* at = slot + rin * D + 32 * d + 8 * e + 4 * half;
-        put2(at, o[d][4 * e], o[d][4 * e + 1]);
-        put2(at + 2, o[d][4 * e + 2], o[d][4 * e + 3]);
-      }
+      for (int e = 0; e < 8; ++e) put2(slot + 2 * ((8 * d + e) * 64 * NW + tid), o[d][2 * e], o[d][2 * e + 1]);
     if (half == 0) put2(slot + BM * D + 2 * rin, m, all);
+    __shared__ uint32_t last;
+    if (!last_to_arrive(p.tickets + (int64_t)block * p.c.heads + h, ns, tid, &last)) return;
+    const float* stat = slot0 + BM * D + 2 * rin;
+    m = -FLT_MAX;
+    for (int u = 0; u < ns; ++u) m = fmaxf(m, get2(stat + (int64_t)u * SLOT)[0]);
+    all = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
+    for (int u = 0; u < ns; ++u) {
+      const v2f st = get2(stat + (int64_t)u * SLOT);
+      const float f = exp2_fast(st[0] - m);
+      all += f * st[1];
+      const float* src = slot0 + (int64_t)u * SLOT + 2 * tid;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        v2f x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = get2(src + 2 * (8 * d + e) * 64 * NW);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          o[d][2 * e] += f * x[e][0];
+          o[d][2 * e + 1] += f * x[e][1];
+        }
+      }
+    }
   }
-  __shared__ uint32_t last;
-  if (!last_to_arrive(p.tickets + (int64_t)block * p.c.heads + h, ns, tid, &last)) return;
-  static_assert(BM * (kMaxTileSlices + 1) * 4 <= sizeof(lds), "the slices' weights");
-  join_slices<DT, D, BM, 64 * NW>(p, k, h, ns, slot0, (float*)lds, tok0, vs, tid);
+  if (!live) return;
+  const float f = row_factor(all, vs);
+  char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (int64_t)(h * G + g) * p.ldoh;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *(u2*)(dst + 2 * (32 * d + 8 * e + 4 * half)) = (u2){pack16<DT>(o[d][4 * e] * f, o[d][4 * e + 1] * f),
+                                                           pack16<DT>(o[d][4 * e + 2] * f, o[d][4 * e + 3] * f)};
+  if (p.lse && half == 0) p.lse[(int64_t)(tok0 + i) * p.q_heads + h * G + g] = row_lse(m, all);
 }
 
 template <int DT, bool F8, int D>
