@@ -16,40 +16,54 @@ struct AttnParams {
   int q_heads, group, window;
   float scale;
   int rows_from, rows_to; // sequences with rows_from <= n G < rows_to are this kernel's
-  int slices, slice_keys; // most slices of a sequence's keys, keys of one (a multiple of 256)
-  uint32_t* tickets;      // [row blocks][key heads]: slices done, zero between calls
-  float* part;            // [row blocks][key heads][slices]: the slots where slices meet
+  int slices, slice_keys; // tile kernel: most slices of a sequence's keys, keys of one (a multiple of 64); few: 1, or more, and keys of a share at least
+  uint32_t* tickets;      // slices done, zero between calls: [row blocks][key heads]; few: [workgroups]
+  float* part;            // the slots where slices meet: [row blocks][key heads][slices]; few: [workgroups][2]
   KvView c;
 };
 
 struct RowBlock {
-  int b, r0, n, L;        // sequence, first row, new tokens, keys
+  int b, tok0, r0, n, L;  // sequence, its first row of q, the block's first row, new tokens, keys
   int rows;               // rows of the block (<= 0: none)
   int begin, end;         // keys that any of its rows sees: begin <= j < end
 };
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-// Block `block` of BM rows.  WHOLE: every sequence that is this kernel's fits one, and the block's number is the sequence's.  Else sequence b has the
-// blocks from floor(cu[b] G / BM) + b on, up to where sequence b + 1's begin: at least as many as it needs, in a place that takes no sum over the
-// sequences before it.
-template <int BM, bool WHOLE>
-__device__ __forceinline__ RowBlock row_block(const AttnParams& p, int block, int lane) {
+// The block of BM rows from r0 on of sequence b, whose new tokens are rows c0 .. c0+n-1 of q and which has L keys.
+template <int BM>
+__device__ __forceinline__ RowBlock row_block_at(const AttnParams& p, int b, int c0, int n, int L, int r0) {
   RowBlock k;
   const int G = p.group;
-  k.rows = 0;
-  k.b = WHOLE ? block : sequences_before(block, p.c.seqs, lane, [&](int i) { return p.c.cu[i + 1] * G / BM + i + 1; });
-  if (k.b >= p.c.seqs) return k;
-  const int c0 = uniform(p.c.cu[k.b]), c1 = uniform(p.c.cu[k.b + 1]);
-  k.n = c1 - c0;
-  k.L = uniform(p.c.len[k.b]);
-  k.r0 = WHOLE ? 0 : (block - (c0 * G / BM + k.b)) * BM;
-  if (k.n <= 0 || k.n * G < p.rows_from || k.n * G >= p.rows_to || c0 < 0 || c1 > p.c.tokens) return k;
-  k.rows = min(k.n * G - k.r0, BM);
-  if (k.rows <= 0) return k;
-  const int first = k.L - k.n + k.r0 / G, last = k.L - k.n + (k.r0 + k.rows - 1) / G;
+  k.b = b;
+  k.tok0 = c0;
+  k.n = n;
+  k.L = L;
+  k.r0 = r0;
+  k.rows = min(n * G - r0, BM);
+  const int first = L - n + r0 / G, last = L - n + (r0 + k.rows - 1) / G;
   k.end = min(last + 1, p.c.width << p.c.page_shift);
   k.begin = p.window > 0 ? max(0, first - p.window + 1) : 0;
   return k;
 }
+// whether a sequence is this kernel's (and one that can be)
+__device__ __forceinline__ bool takes(const AttnParams& p, int c0, int n) {
+  return n > 0 && c0 >= 0 && n <= p.c.tokens - c0 && n * p.group >= p.rows_from && n * p.group < p.rows_to;
+}
+// Block `block` of BM rows: sequence b has the blocks from floor(cu[b] G / BM) + b on, up to where sequence b + 1's begin: at least as many as it
+// needs, in a place that takes no sum over the sequences before it.
+template <int BM>
+__device__ __forceinline__ RowBlock row_block(const AttnParams& p, int block, int lane) {
+  RowBlock none;
+  none.rows = 0;
+  const int b = sequences_before(block, p.c.seqs, lane, [&](int i) { return p.c.cu[i + 1] * p.group / BM + i + 1; });
+  if (b >= p.c.seqs) return none;
+  const int c0 = uniform(p.c.cu[b]), n = uniform(p.c.cu[b + 1]) - c0;
+  if (!takes(p, c0, n)) return none;
+  return row_block_at<BM>(p, b, c0, n, uniform(p.c.len[b]), (block - (c0 * p.group / BM + b)) * BM);
+}
+
+// device memory behind an address that is put together from numbers (a plain pointer would be taken for one that may also point into LDS)
+typedef __attribute__((address_space(1))) const char GlobalByte;
+typedef __attribute__((address_space(1))) const u4 GlobalPiece;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // an ulp; below 2^-126 to zero
 
@@ -101,7 +115,7 @@ __device__ __forceinline__ float row_lse(float m, float l) {
   return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.693147180559945309f;
 }
 
-constexpr int kMaxSlices = 128;          // of the kernel for few rows
+constexpr int kMaxSlices = 256;          // of the kernel for few rows
 constexpr int kMaxTileSlices = 32;       // of the kernel for many
 constexpr int kTileRows = 128;
 constexpr float kLog2e = 1.44269504088896341f;
@@ -131,7 +145,8 @@ __device__ __forceinline__ bool last_to_arrive(uint32_t* ticket, int ns, int tid
   return *shared == (uint32_t)(ns - 1);
 }
 size_t paged_attn_few_slot_floats(int nb, int D);
-int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, hipStream_t st);
+int paged_attn_few_resident(int nb, bool f8, int D);          // workgroups that a compute unit runs together
+int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, int workgroups, hipStream_t st);
 size_t paged_attn_tile_slot_floats(int D);
 int launch_paged_attn_tile(const AttnParams& p, int dtype, bool f8, int D, int blocks, hipStream_t st);
 

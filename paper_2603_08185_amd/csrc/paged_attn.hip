@@ -8,6 +8,7 @@ constexpr int kTickets = 4096;                                // words at the st
 
 // Sequences with more rows than this go to the kernel for many.
 constexpr int kFewRows = 32;
+constexpr int kFewKeys = 256;                                 // keys of a share of the kernel for few rows, at least
 
 // (rows fit 31 bits, the threads of a grid 32)
 bool counts_ok(int64_t tokens, int64_t seqs, int q_heads, int heads) {
@@ -41,7 +42,7 @@ struct Plans {
   Plan f, m;
 };
 
-Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int heads, int group, int D) {
+Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int heads, int group, int D, bool f8) {
   Plans k{};
   if (max_q > tokens) max_q = (int)tokens;
   const int64_t rows = (int64_t)max_q * group;
@@ -52,7 +53,14 @@ Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int
   const int64_t cus = device_cu_count();
   if (k.few) {
     k.nb = rows <= 16 ? 1 : 2;
-    k.f = plan(seqs, heads, keys, 4 * cus, kMaxSlices, 256, paged_attn_few_slot_floats(k.nb, D));
+    // as many workgroups as run together, each with an equal share of a head's keys; many more sequences than that are even enough by themselves
+    const int64_t together = cus * paged_attn_few_resident(k.nb, f8, D), whole = (int64_t)seqs * heads;
+    k.f = Plan{(int)whole, 1, 0, 16};
+    if (whole < 16 * together && (together + heads - 1) / heads * heads <= kTickets) {
+      const int64_t most = seqs * ((keys + kFewKeys - 1) / kFewKeys + 1), each = (together + heads - 1) / heads;
+      k.f = Plan{(int)(each < most ? each : most) * heads, 2, kFewKeys, 0};
+      k.f.bytes = kTickets * 4 + (size_t)k.f.blocks * 2 * paged_attn_few_slot_floats(k.nb, D) * 4;
+    }
   }
   if (k.many) {
     const int blocks = (int)(tokens * group / kTileRows) + seqs;
@@ -72,7 +80,7 @@ size_t serq_paged_attn_workspace_bytes(int64_t tokens, int seqs, int max_q, int6
   if (tokens < 0 || tokens > kKvTokens || seqs < 0 || seqs > 65536 || max_q < 0 || max_kv < 0 || kv_heads < 1 || kv_heads > 1024 ||
       q_heads < 1 || q_heads > 65535 || q_heads % kv_heads || (dim != 64 && dim != 128) || !counts_ok(tokens, seqs, q_heads, kv_heads))
     return 0;
-  const Plans k = plans(tokens, seqs, max_q, max_kv, 0, kv_heads, q_heads / kv_heads, dim);
+  const Plans k = plans(tokens, seqs, max_q, max_kv, 0, kv_heads, q_heads / kv_heads, dim, false);
   return k.f.bytes > k.m.bytes ? k.f.bytes : k.m.bytes;       // (the two kernels of a call follow each other)
 }
 
@@ -94,7 +102,7 @@ int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int d
   p.q = (const char*)q; p.out = (char*)out; p.lse = lse;
   p.ldq = 2 * ldq; p.ldqh = 2 * ldqh; p.ldo = 2 * ldo; p.ldoh = 2 * ldoh;
   p.q_heads = q_heads; p.group = q_heads / cache->heads; p.window = window; p.scale = scale;
-  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, window, cache->heads, p.group, D);
+  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, window, cache->heads, p.group, D, cache->dtype == SERQ_F8);
   const auto place = [&](const Plan& n) {
     const bool sliced = n.slices > 1 && workspace && workspace_bytes >= n.bytes;
     p.slices = sliced ? n.slices : 1;
@@ -114,7 +122,7 @@ int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int d
     p.rows_from = 0;
     p.rows_to = k.many ? kFewRows + 1 : 0x7fffffff;
     place(k.f);
-    rc = launch_paged_attn_few(p, dtype, f8, D, k.nb, (hipStream_t)stream);
+    rc = launch_paged_attn_few(p, dtype, f8, D, k.nb, p.slices > 1 ? k.f.blocks : p.c.seqs * p.c.heads, (hipStream_t)stream);
   }
   return rc;
 }

@@ -1,8 +1,10 @@
 // serq_paged_attn for sequences with few rows (a token or a few, times the query heads of a key head): the cache is read once, and
 // everything else is there to keep it coming.
 //
-// A workgroup takes 16 NB rows, a key head and a slice of the keys; each of its four waves takes every fourth tile of 16 TG keys and walks alone,
-// with a running maximum, sum and weighted values of its own; the four meet in LDS at the end, and the slices of a sequence in the
+// The keys that the call's sequences see form a line for each key head that is cut into equal shares, one a workgroup, so that neither few
+// sequences nor sequences of very different lengths leave compute units idle.  A workgroup walks the stretches of its share: a sequence's
+// 16 NB rows of the key head and some of its keys.  Each of its four waves takes every fourth tile of 16 TG keys and walks alone, with a running
+// maximum, sum and weighted values of its own; the four meet in LDS at the stretch's end, and the stretches of a sequence that was cut in the
 // workspace, where the last one to arrive joins them.
 //   scores   S^T = K Q^T on the 16x16x32 matrix instruction: keys are its rows, fetched from memory in the layout of its operand (a lane has
 //            16 bytes of one key), queries its columns, so that a lane's results are 4 keys of one row.
@@ -11,6 +13,8 @@
 //   values   O^T = V^T P^T: the lane's weights are the instruction's operand as they stand (8 keys: 4 of one group of 16, 4 of the next); V goes
 //            through LDS, which reads it back by columns.
 // Weights are rounded to the 16-bit type for the product; their sum takes them unrounded.
+#include <type_traits>
+
 #include "paged_attn.h"
 
 namespace serq {
@@ -18,13 +22,16 @@ namespace {
 
 constexpr int kWaves = 4;
 
-template <bool F8, int D> struct Few {
+template <bool F8, int D, int NB> struct Few {
   static constexpr int ROWB = D * (F8 ? 1 : 2);               // bytes of a key in the cache
-  static constexpr int TG = ROWB == 256 ? 2 : 4;              // groups of 16 keys in a tile
+  static constexpr int TG = ROWB == 256 || (F8 && D == 128 && NB == 2) ? 2 : 4;   // groups of 16 keys in a tile (the second: registers)
   static constexpr int KEYS = 16 * TG;
   static constexpr int KL = ROWB / 64;                        // 16-byte loads of a lane for 16 keys
   static constexpr int LPR = ROWB / 16, RPI = 64 / LPR;       // V: lanes of a row, rows of a load
   static constexpr int STEPS = D / 32;
+  static constexpr int OPITCH = D + 4;                        // floats of a row where the waves meet
+  // LDS of a wave: a tile of V, then its rows' sums
+  static constexpr int REGION = KEYS * D * 2 > 16 * NB * OPITCH * 4 ? KEYS * D * 2 : 16 * NB * OPITCH * 4;
 };
 
 template <int DT>
@@ -39,11 +46,10 @@ __device__ __forceinline__ v4f mfma(const u4& a, const u4& b, const v4f& c) {
 template <int D>
 __device__ __forceinline__ int turned(int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); }
 
-// The ns slots from slot0 on, joined and written out.  scratch: rows x (ns + 1) floats of LDS.
-template <int DT, int D, int BM, int THREADS>
-__device__ __forceinline__ void join_slices(const AttnParams& p, const RowBlock& k, int h, int ns, const float* slot0, float* scratch, int tok0,
+// The slots slot(0) .. slot(ns - 1), joined in this order and written out.  scratch: rows x (ns + 1) floats of LDS.
+template <int DT, int D, int BM, int THREADS, class Slot>
+__device__ __forceinline__ void join_slices(const AttnParams& p, const RowBlock& k, int h, int ns, const Slot& slot, float* scratch, int tok0,
                                             float vs, int tid) {
-  constexpr int SLOT = BM * (D + 2);
   const int l = tid & 63, w = uniform(tid >> 6);
   float* weight = scratch + BM;                               // [rows][ns]: each slice's weight; scratch[row]: what the row is multiplied by
   for (int r = w; r < k.rows; r += THREADS / 64) {
@@ -54,7 +60,7 @@ __device__ __forceinline__ void join_slices(const AttnParams& p, const RowBlock&
       m[e] = -FLT_MAX;
       n[e] = 0.0f;
       if (u < ns) {
-        const v2f x = get2(slot0 + (int64_t)u * SLOT + BM * D + 2 * r);
+        const v2f x = get2(slot(u) + BM * D + 2 * r);
         m[e] = x[0];
         n[e] = x[1];
       }
@@ -82,16 +88,17 @@ __device__ __forceinline__ void join_slices(const AttnParams& p, const RowBlock&
   for (int it = tid; it < k.rows * (D / 2); it += THREADS) {
     const int r = it / (D / 2), d = 2 * (it % (D / 2));
     v2f acc = {0.0f, 0.0f};
-    const float* src = slot0 + r * D + d;
-    int u = 0;
-    for (; u + 8 <= ns; u += 8) {                             // eight loads under way together
-      v2f x[8];
+    // N loads under way together: a load takes a microsecond here (past the end: the last slot again, without weight)
+    const auto some = [&](int u, auto number) {
+      constexpr int N = decltype(number)::value;
+      v2f x[N];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = get2(src + (int64_t)(u + e) * SLOT);
+      for (int e = 0; e < N; ++e) x[e] = get2(slot(min(u + e, ns - 1)) + r * D + d);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc += weight[r * ns + u + e] * x[e];
-    }
-    for (; u < ns; ++u) acc += weight[r * ns + u] * get2(src + (int64_t)u * SLOT);
+      for (int e = 0; e < N; ++e) acc += (u + e < ns ? weight[r * ns + min(u + e, ns - 1)] : 0.0f) * x[e];
+    };
+    if (ns <= 8) some(0, std::integral_constant<int, 8>{});
+    else for (int u = 0; u < ns; u += 16) some(u, std::integral_constant<int, 16>{});
     const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
     const float f = scratch[r];
     char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (int64_t)(h * p.group + g) * p.ldoh;
@@ -99,31 +106,27 @@ __device__ __forceinline__ void join_slices(const AttnParams& p, const RowBlock&
   }
 }
 
-template <int DT, bool F8, int D, int NB>
-__global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
-  using S = Few<F8, D>;
-  constexpr int TG = S::TG, KEYS = S::KEYS, KL = S::KL, BM = 16 * NB, VL = TG * KL;
-  constexpr int VBYTES = KEYS * D * 2;
-  constexpr int OPITCH = D + 4;                               // floats of a row where the waves meet
-  constexpr int MEET = BM * OPITCH * 4;
-  constexpr int REGION = VBYTES > MEET ? VBYTES : MEET;
-  __shared__ __align__(16) char lds[kWaves * REGION];
-  __shared__ float stat[kWaves][BM][2];
-  __shared__ uint32_t last;
+// A stretch of a sequence that was cut: where the sequence's stretches leave their sums, and how many there are.
+template <int SLOT>
+struct Part {
+  float* base;            // of the workspace's slots, two a workgroup: for a stretch that goes on with a sequence, and for one that begins it
+  uint32_t* ticket;
+  int first, mine, count; // the workgroup that begins the sequence; this stretch's number, all of them
+  __device__ __forceinline__ float* slot(int u) const { return base + (int64_t)(2 * (first + u) + (u == 0)) * SLOT; }
+};
 
-  const int tid = threadIdx.x, l = tid & 63, w = uniform(tid >> 6);
-  const int n16 = l & 15, quad = l >> 4;
-  const int h = blockIdx.y, s = blockIdx.z, G = p.group;
-  const RowBlock k = row_block<BM, true>(p, blockIdx.x, l);
-  if (k.rows <= 0) return;
-  const int base = k.begin & ~15;
-  // (more keys than the slices were made for: the last one takes them)
-  const int ns = k.end > base ? min((k.end - base - 1) / p.slice_keys + 1, p.slices) : 1;
-  if (s >= ns) return;
-  const int k0 = base + s * p.slice_keys, k1 = s == ns - 1 ? k.end : k0 + p.slice_keys;
+// Keys k0 .. k1-1 for the rows of block k and key head h.
+template <int DT, bool F8, int D, int NB>
+__device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, int h, int k0, int k1, const bool cut,
+                                        const Part<16 * NB * (D + 2)> part, char* lds, float (*stat)[16 * NB][2]) {
+  using S = Few<F8, D, NB>;
+  constexpr int TG = S::TG, KEYS = S::KEYS, KL = S::KL, BM = 16 * NB, VL = TG * KL, OPITCH = S::OPITCH, REGION = S::REGION;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));                               // (else what follows from it is kept from stretch to stretch: 67 registers)
+  const int l = tid & 63, w = uniform(tid >> 6);
+  const int n16 = l & 15, quad = l >> 4, G = p.group, tok0 = k.tok0;
 
   // the rows' queries, and the keys that each sees: lo <= j < hi
-  const int tok0 = uniform(p.c.cu[k.b]);
   u4 q[NB][S::STEPS];
   int lo[NB], hi[NB];
 #pragma unroll
@@ -152,35 +155,47 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
   const char* kbase = p.c.k + h * p.c.k_head;
   const char* vbase = p.c.v + h * p.c.v_head;
   const uint32_t klane = (uint32_t)(n16 * (int)p.c.k_token + quad * 16);
-  const uint32_t vlane = (uint32_t)((l / S::LPR) * (int)p.c.v_token + (l % S::LPR) * 16);
+  uint32_t vlane[KL];
+#pragma unroll
+  for (int i = 0; i < KL; ++i) vlane[i] = (uint32_t)((i * S::RPI + l / S::LPR) * (int)p.c.v_token + (l % S::LPR) * 16);
 
   const int nt = k1 > k0 ? (k1 - k0 + KEYS - 1) / KEYS : 0;   // tiles of the slice
   const int mine = nt > w ? (nt - w + kWaves - 1) / kWaves : 0;
-  // page numbers of the wave's next 64 / TG tiles, one group of 16 keys a lane (past the end: the last key's page)
-  int pages = 0;
+  // lane: where group lane % TG of the wave's tile lane / TG of the next 64 / TG begins, so that a tile's loads need no arithmetic of their own
+  // (past the end: in the last key's page)
+  uint64_t kfrom = 0, vfrom = 0;
   auto look_up = [&](int t) {
-    const int key = min(k0 + (w + kWaves * (t + l / TG)) * KEYS + 16 * (l % TG), k.end - 1);
-    pages = min(max(table[key >> p.c.page_shift], 0), p.c.pages - 1);
+    const int key = k0 + (w + kWaves * (t + l / TG)) * KEYS + 16 * (l % TG);
+    const int page = min(max(table[min(key, k.end - 1) >> p.c.page_shift], 0), p.c.pages - 1);
+    kfrom = (uint64_t)(kbase + page * p.c.k_page + (key & mask) * p.c.k_token);
+    vfrom = (uint64_t)(vbase + page * p.c.v_page + (key & mask) * p.c.v_token);
+  };
+  const auto group = [&](uint64_t v, int t, int a) {
+    const int at = (t * TG + a) & 63;
+    const uint32_t lo32 = __builtin_amdgcn_readlane((uint32_t)v, at), hi32 = __builtin_amdgcn_readlane((uint32_t)(v >> 32), at);
+    return (const GlobalByte*)((uint64_t)hi32 << 32 | lo32);
   };
   u4 kr[TG][KL], vr[VL];
   auto load_k = [&](int t) {
-    const int key0 = k0 + (w + kWaves * t) * KEYS;
+    uint32_t lane = klane;
+    asm("" : "+v"(lane));                                     // (an offset of 32 bits beside a uniform address; else kept as one of 64 bits)
 #pragma unroll
     for (int a = 0; a < TG; ++a) {
-      const int pg = __builtin_amdgcn_readlane(pages, (t * TG + a) & 63);
-      const char* row = kbase + pg * p.c.k_page + ((key0 + 16 * a) & mask) * p.c.k_token;
+      const GlobalByte* row = group(kfrom, t, a);
 #pragma unroll
-      for (int i = 0; i < KL; ++i) kr[a][i] = *(const u4*)(row + klane + 64 * i);
+      for (int i = 0; i < KL; ++i) kr[a][i] = __builtin_nontemporal_load((const GlobalPiece*)(row + lane + 64 * i));
     }
   };
   auto load_v = [&](int t) {
-    const int key0 = k0 + (w + kWaves * t) * KEYS;
 #pragma unroll
     for (int a = 0; a < TG; ++a) {
-      const int pg = __builtin_amdgcn_readlane(pages, (t * TG + a) & 63);
-      const char* row = vbase + pg * p.c.v_page + ((key0 + 16 * a) & mask) * p.c.v_token;
+      const GlobalByte* row = group(vfrom, t, a);
 #pragma unroll
-      for (int i = 0; i < KL; ++i) vr[a * KL + i] = *(const u4*)(row + i * S::RPI * p.c.v_token + vlane);
+      for (int i = 0; i < KL; ++i) {
+        uint32_t lane = vlane[i];
+        asm("" : "+v"(lane));
+        vr[a * KL + i] = __builtin_nontemporal_load((const GlobalPiece*)(row + lane));
+      }
     }
   };
 
@@ -209,8 +224,10 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
     load_k(0);
     load_v(0);
   }
-#pragma unroll 1
-  for (int t = 0; t < mine; ++t) {
+  // One tile.  The loads of the next one are sent without a condition (the waits count loads: one that may not have been sent counts as none,
+  // and the wait for K would be one for V too), so the last tile is a case of its own.
+  const auto tile = [&](int t, auto more) {
+    constexpr bool MORE = decltype(more)::value;
     const int key0 = k0 + (w + kWaves * t) * KEYS;
     // scores
     v4f sc[TG][NB];
@@ -229,20 +246,21 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
         for (int st = 0; st < S::STEPS; ++st) sc[a][nb] = mfma<DT>(kk[st], q[nb][st], sc[a][nb]);
       }
     }
-    const bool more = t + 1 < mine;
-    if (more) {
+    if constexpr (MORE) {
       if (((t + 1) * TG & 63) == 0) look_up(t + 1);
       load_k(t + 1);
     }
     __builtin_amdgcn_sched_barrier(0);
     // V to LDS; rows that no row sees are zero there (a weight of zero does not make NaN zero)
     const bool ends = key0 < k.begin || key0 + KEYS > k.end;
+    int to = vrow * D * 2, turn = cturn;
+    asm volatile("" : "+v"(to), "+v"(turn));                   // (else sixteen places in LDS are kept from tile to tile)
 #pragma unroll
     for (int u = 0; u < VL; ++u) {
       const int row = u * S::RPI + vrow;
       u4 x = vr[u];
       if (ends && (key0 + row < k.begin || key0 + row >= k.end)) x = (u4){0, 0, 0, 0};
-      char* at = my + row * D * 2;
+      char* at = my + u * S::RPI * D * 2 + to;
       if constexpr (F8) {
         u4 a, b;
         widen_e4m3<DT>(x, a, b);
@@ -253,7 +271,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
         *(u4*)(at + ((vpiece ^ turned<D>(row)) << 4)) = x;
       }
     }
-    if (more) load_v(t + 1);
+    if constexpr (MORE) load_v(t + 1);
     __builtin_amdgcn_sched_barrier(0);
     // weights
     if (key0 < all_lo || key0 + KEYS > all_hi) {
@@ -301,13 +319,16 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
     for (int st = 0; st < TG / 2; ++st)
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) {
-        const char* at = col + st * 32 * D * 2 + ((2 * d << 4) ^ cturn);
+        const char* at = col + st * 32 * D * 2 + ((2 * d << 4) ^ turn);
         const u2 x = lds_column4(at), y = lds_column4(at + 16 * D * 2);
         const u4 a = {x.x, x.y, y.x, y.y};
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) o[nb][d] = mfma<DT>(a, pw[nb][st], o[nb][d]);
       }
-  }
+  };
+#pragma unroll 1
+  for (int t = 0; t < mine - 1; ++t) tile(t, std::true_type{});
+  if (mine > 0) tile(mine - 1, std::false_type{});
 
   // the waves meet
 #pragma unroll
@@ -323,9 +344,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
   }
   __syncthreads();
   const int64_t head0 = (int64_t)h * G;
-  const bool sliced = ns > 1;                                 // the slices of a sequence meet in the workspace
-  float* slot0 = p.part + ((int64_t)blockIdx.x * p.c.heads + h) * p.slices * (BM * (D + 2));
-  float* slot = slot0 + (int64_t)s * (BM * (D + 2));
+  float* slot = cut ? part.slot(part.mine) : nullptr;
   for (int it = tid; it < k.rows * (D / 4); it += 256) {
     const int r = it / (D / 4), d = 4 * (it % (D / 4));
     float top = stat[0][r][0];
@@ -339,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
       all += f * stat[u][r][1];
       acc += f * *(const v4f*)((const float*)(lds + u * REGION) + r * OPITCH + d);
     }
-    if (sliced) {
+    if (cut) {
       put2(slot + r * D + d, acc[0], acc[1]);
       put2(slot + r * D + d + 2, acc[2], acc[3]);
       if (d == 0) put2(slot + BM * D + 2 * r, top, all);
@@ -351,16 +370,96 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
       if (p.lse && d == 0) p.lse[(int64_t)(tok0 + i) * p.q_heads + head0 + g] = row_lse(top, all);
     }
   }
-  if (!sliced) return;
+  if (!cut) return;
+  __shared__ uint32_t last;
+  if (!last_to_arrive(part.ticket, part.count, tid, &last)) return;
+  static_assert(BM * (kMaxSlices + 1) * 4 <= kWaves * REGION, "the stretches' weights");
+  join_slices<DT, D, BM, 256>(p, k, h, part.count, [&](int u) { return part.slot(u); }, (float*)lds, tok0, vs, tid);   // (the regions of the waves are free)
+}
 
-  if (!last_to_arrive(p.tickets + (int64_t)blockIdx.x * p.c.heads + h, ns, tid, &last)) return;
-  static_assert(BM * (kMaxSlices + 1) * 4 <= kWaves * REGION, "the slices' weights");
-  join_slices<DT, D, BM, 256>(p, k, h, ns, slot0, (float*)lds, tok0, vs, tid);   // (the regions of the waves are free)
+// What a lane knows of a sequence: its new tokens, its keys, and the blocks of 64 keys that it gives a key head to do: none if it is not this
+// kernel's, at least one else (its rows have to be written).
+constexpr int kUnit = 64;
+struct Sequence { int c0, n, L, blocks; };
+__device__ __forceinline__ Sequence sequence(const AttnParams& p, int b) {
+  Sequence s{p.c.cu[b], 0, p.c.len[b], 0};
+  s.n = p.c.cu[b + 1] - s.c0;
+  if (takes(p, s.c0, s.n)) {
+    const int end = min(s.L, p.c.width << p.c.page_shift), base = (p.window > 0 ? max(0, s.L - s.n - p.window + 1) : 0) & ~15;
+    s.blocks = end > base ? (end - base - 1) / kUnit + 1 : 1;
+  }
+  return s;
+}
+// sum over the lanes up to each one
+__device__ __forceinline__ int sum_upto(int v, int lane) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);     // 1, 2, 4 and 8 lanes before, within 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  const int a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47);
+  return v + (lane >= 48 ? a + b + c : lane >= 32 ? a + b : lane >= 16 ? a : 0);
+}
+
+template <int DT, bool F8, int D, int NB>
+__global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
+  using S = Few<F8, D, NB>;
+  constexpr int BM = 16 * NB;
+  __shared__ __align__(16) char lds[kWaves * S::REGION];
+  __shared__ float stat[kWaves][BM][2];
+  const int l = threadIdx.x & 63, heads = p.c.heads;
+  // neighbouring workgroups have different key heads
+  const int number = uniform(blockIdx.x / heads), h = blockIdx.x - number * heads;
+  if (p.slices <= 1) {                                        // nowhere to meet: a workgroup takes a sequence whole
+    const int c0 = uniform(p.c.cu[number]), n = uniform(p.c.cu[number + 1]) - c0;
+    if (!takes(p, c0, n)) return;
+    const RowBlock k = row_block_at<BM>(p, number, c0, n, uniform(p.c.len[number]), 0);
+    stretch<DT, F8, D, NB>(p, k, h, k.begin & ~15, max(k.end, 0), false, {}, lds, stat);
+    return;
+  }
+  // Every wave for itself: a lane counts the blocks of some sequences, and knows what lies before them.
+  const int per = (p.c.seqs + 63) / 64, b0 = l * per;
+  Sequence s{};                                               // the last that the lane looked at
+  int own = 0;
+  for (int i = min(per, p.c.seqs - b0) - 1; i >= 0; --i) {    // (the first one last)
+    s = sequence(p, b0 + i);
+    own += s.blocks;
+  }
+  const int upto = sum_upto(own, l), total = __builtin_amdgcn_readlane(upto, 63);
+  // a share: of the head's line, but not too little for a workgroup, nor so little that too many meet
+  const int wanted = gridDim.x / heads;
+  const int share = max(max(p.slice_keys / kUnit, total / (kMaxSlices - 2) + 1), (total + wanted - 1) / wanted);
+  int at = (int)min((int64_t)number * share, (int64_t)total);
+  const int stop = min(at + share, total);
+  while (at < stop) {
+    const int lane = __builtin_ctzll(__ballot(own > 0 && at >= upto - own && at < upto));
+    int b = b0, from = upto - own;
+    if (l == lane && own > s.blocks) {                        // several sequences: which of them
+      s = sequence(p, b);
+      while (at >= from + s.blocks) {
+        from += s.blocks;
+        s = sequence(p, ++b);
+      }
+    }
+    const RowBlock k = row_block_at<BM>(p, __builtin_amdgcn_readlane(b, lane), __builtin_amdgcn_readlane(s.c0, lane),
+                                        __builtin_amdgcn_readlane(s.n, lane), __builtin_amdgcn_readlane(s.L, lane), 0);
+    const int begins = __builtin_amdgcn_readlane(from, lane), ends = begins + __builtin_amdgcn_readlane(s.blocks, lane);
+    const int until = min(stop, ends), base = k.begin & ~15;
+    const bool cut = at > begins || until < ends;
+    const int k0 = base + (at - begins) * kUnit, k1 = until < ends ? base + (until - begins) * kUnit : max(k.end, 0);
+    Part<BM * (D + 2)> part{};
+    if (cut) {
+      const int first = begins / share;
+      part = {p.part + (int64_t)h * wanted * 2 * (BM * (D + 2)), p.tickets + h * wanted + first, first, number - first, (ends - 1) / share - first + 1};
+    }
+    stretch<DT, F8, D, NB>(p, k, h, k0, k1, cut, part, lds, stat);
+    at = until;
+    __syncthreads();                                          // LDS is free again
+  }
 }
 
 template <int DT, bool F8, int D>
-int launch(const AttnParams& p, int nb, hipStream_t st) {
-  const dim3 grid((unsigned)p.c.seqs, (unsigned)p.c.heads, (unsigned)p.slices);
+int launch(const AttnParams& p, int nb, int workgroups, hipStream_t st) {
+  const dim3 grid((unsigned)workgroups);
   if (nb == 1) hipLaunchKernelGGL((paged_attn_few_kernel<DT, F8, D, 1>), grid, dim3(256), 0, st, p);
   else hipLaunchKernelGGL((paged_attn_few_kernel<DT, F8, D, 2>), grid, dim3(256), 0, st, p);
   return hipGetLastError() == hipSuccess ? SERQ_OK : SERQ_EHIP;
@@ -369,15 +468,16 @@ int launch(const AttnParams& p, int nb, hipStream_t st) {
 }  // namespace
 
 size_t paged_attn_few_slot_floats(int nb, int D) { return (size_t)16 * nb * (D + 2); }
+int paged_attn_few_resident(int nb, bool f8, int D) { return D == 64 && f8 && nb == 1 ? 3 : 2; }
 
-int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, hipStream_t st) {
+int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, int workgroups, hipStream_t st) {
   const bool bf = dtype == SERQ_BF16;
   if (D == 128) {
-    if (bf) return f8 ? launch<SERQ_BF16, true, 128>(p, nb, st) : launch<SERQ_BF16, false, 128>(p, nb, st);
-    return f8 ? launch<SERQ_F16, true, 128>(p, nb, st) : launch<SERQ_F16, false, 128>(p, nb, st);
+    if (bf) return f8 ? launch<SERQ_BF16, true, 128>(p, nb, workgroups, st) : launch<SERQ_BF16, false, 128>(p, nb, workgroups, st);
+    return f8 ? launch<SERQ_F16, true, 128>(p, nb, workgroups, st) : launch<SERQ_F16, false, 128>(p, nb, workgroups, st);
   }
-  if (bf) return f8 ? launch<SERQ_BF16, true, 64>(p, nb, st) : launch<SERQ_BF16, false, 64>(p, nb, st);
-  return f8 ? launch<SERQ_F16, true, 64>(p, nb, st) : launch<SERQ_F16, false, 64>(p, nb, st);
+  if (bf) return f8 ? launch<SERQ_BF16, true, 64>(p, nb, workgroups, st) : launch<SERQ_BF16, false, 64>(p, nb, workgroups, st);
+  return f8 ? launch<SERQ_F16, true, 64>(p, nb, workgroups, st) : launch<SERQ_F16, false, 64>(p, nb, workgroups, st);
 }
 
 }  // namespace serq

@@ -62,13 +62,13 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(AttnParams 
   // the rows that see most keys come last in a sequence and start first; neighbouring workgroups have different key heads
   const int units = gridDim.x / p.c.heads;
   const int h = blockIdx.x % p.c.heads, block = units - 1 - blockIdx.x / p.c.heads, s = blockIdx.z;
-  const RowBlock k = row_block<BM, false>(p, block, l);
+  const RowBlock k = row_block<BM>(p, block, l);
   if (k.rows <= 0) return;
   const int base = k.begin & ~15;
   const int ns = k.end > base ? min((k.end - base - 1) / p.slice_keys + 1, p.slices) : 1;
   if (s >= ns) return;
   const int k0 = base + s * p.slice_keys, k1 = s == ns - 1 ? k.end : k0 + p.slice_keys;
-  const int tok0 = uniform(p.c.cu[k.b]);
+  const int tok0 = k.tok0;
 
   // the lane's row, and the keys that it sees: lo <= j < hi
   const int rin = 32 * w + n32, r = k.r0 + rin;
