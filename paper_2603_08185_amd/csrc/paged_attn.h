@@ -30,7 +30,7 @@ struct RowBlock {
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 // The block of BM rows from r0 on of sequence b, whose new tokens are rows c0 .. c0+n-1 of q and which has L keys.
 template <int BM>
-__device__ __forceinline__ RowBlock row_block_at(const AttnParams& p, int b, int c0, int n, int L, int r0) {
+__device__ __forceinline__ RowBlock row_block(const AttnParams& p, int b, int c0, int n, int L, int r0) {
   RowBlock k;
   const int G = p.group;
   k.b = b;
@@ -48,18 +48,65 @@ __device__ __forceinline__ RowBlock row_block_at(const AttnParams& p, int b, int
 __device__ __forceinline__ bool takes(const AttnParams& p, int c0, int n) {
   return n > 0 && c0 >= 0 && n <= p.c.tokens - c0 && n * p.group >= p.rows_from && n * p.group < p.rows_to;
 }
-// Block `block` of BM rows: sequence b has the blocks from floor(cu[b] G / BM) + b on, up to where sequence b + 1's begin: at least as many as it
-// needs, in a place that takes no sum over the sequences before it.
-template <int BM>
-__device__ __forceinline__ RowBlock row_block(const AttnParams& p, int block, int lane) {
-  RowBlock none;
-  none.rows = 0;
-  const int b = sequences_before(block, p.c.seqs, lane, [&](int i) { return p.c.cu[i + 1] * p.group / BM + i + 1; });
-  if (b >= p.c.seqs) return none;
-  const int c0 = uniform(p.c.cu[b]), n = uniform(p.c.cu[b + 1]) - c0;
-  if (!takes(p, c0, n)) return none;
-  return row_block_at<BM>(p, b, c0, n, uniform(p.c.len[b]), (block - (c0 * p.group / BM + b)) * BM);
+// sum over the lanes up to each one
+__device__ __forceinline__ int sum_upto(int v, int lane) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);     // 1, 2, 4 and 8 lanes before, within 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  const int a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47);
+  return v + (lane >= 48 ? a + b + c : lane >= 32 ? a + b : lane >= 16 ? a : 0);
 }
+
+// A sequence: its first row of q, its new tokens, its keys, how many pieces of work it gives a key head, and how many those before it give.
+struct Sequence { int b, c0, n, L, pieces, before; };
+
+// The pieces of all sequences in a line.  Every wave for itself: a lane counts those of some sequences, and knows what lies before them.
+// `count(c0, n, L)`: pieces of a sequence that is this kernel's.
+template <class Count>
+struct Line {
+  const AttnParams& p;
+  const Count& count;
+  int l, b0, own, upto, total;
+  Sequence s;                                                 // the lane's: the last that it looked at
+  __device__ __forceinline__ void look(int b) {
+    s.b = b;
+    s.c0 = p.c.cu[b];
+    s.n = p.c.cu[b + 1] - s.c0;
+    s.L = p.c.len[b];
+    s.pieces = takes(p, s.c0, s.n) ? count(s.c0, s.n, s.L) : 0;
+  }
+  __device__ __forceinline__ Line(const AttnParams& q, const Count& c, int lane) : p(q), count(c), l(lane), own(0), s{} {
+    const int per = (p.c.seqs + 63) / 64;
+    b0 = l * per;
+    for (int i = min(per, p.c.seqs - b0) - 1; i >= 0; --i) {  // (the first one last)
+      look(b0 + i);
+      own += s.pieces;
+    }
+    upto = sum_upto(own, l);
+    total = __builtin_amdgcn_readlane(upto, 63);
+  }
+  // the sequence that piece `at` (0 <= at < total) is of
+  __device__ __forceinline__ Sequence find(int at) {
+    const int lane = __builtin_ctzll(__ballot(own > 0 && at >= upto - own && at < upto));
+    int before = upto - own;
+    if (l == lane && own > s.pieces) {                        // several sequences: which of them
+      look(b0);
+      while (at >= before + s.pieces) {
+        before += s.pieces;
+        look(s.b + 1);
+      }
+    }
+    Sequence x;
+    x.b = __builtin_amdgcn_readlane(s.b, lane);
+    x.c0 = __builtin_amdgcn_readlane(s.c0, lane);
+    x.n = __builtin_amdgcn_readlane(s.n, lane);
+    x.L = __builtin_amdgcn_readlane(s.L, lane);
+    x.pieces = __builtin_amdgcn_readlane(s.pieces, lane);
+    x.before = __builtin_amdgcn_readlane(before, lane);
+    return x;
+  }
+};
 
 // device memory behind an address that is put together from numbers (a plain pointer would be taken for one that may also point into LDS)
 typedef __attribute__((address_space(1))) const char GlobalByte;

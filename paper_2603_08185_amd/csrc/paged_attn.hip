@@ -21,18 +21,32 @@ struct Plan {
   size_t bytes;
 };
 
-// Blocks of rows times key heads are the workgroups; while there are fewer than `want`, the keys (at most `keys` that a row block sees) are cut into
-// slices of at least `least` keys.
-Plan plan(int blocks, int heads, int64_t keys, int64_t want, int most, int least, size_t slot_floats) {
+// The kernel for many rows: blocks of rows times key heads are the workgroups; where they would leave compute units idle, the keys (at most `keys` that
+// a row block sees) are cut into slices.  Taken is the number of slices with the shortest time.  A tile of 64 keys takes a workgroup about 1 us, or
+// 1.85 where two share a compute unit (which they do as soon as there are nearly as many as units); to begin takes 5 tiles' time, to begin
+// and to meet 12.  `blocks` counts a block more for each sequence than may be needed; `full` is what there is at least.
+// Measured (32 query and 8 key heads; us with 1 / 2 / 3 / 4 / 5 / 8 slices): 384 tokens after 3500 66.6 / 43.1 / 44.8 / 45.5 / 45.2 / 48.4, 256 after
+// 8000 131.7 / 75.5 / 56.2 / 62.1 / 61.0 / 60.0, 100 after 30000 469 / 245 / 171 / 134 / 114 / 87, 512 fresh ones 14.9 / 16.9 / 17.3 / 21.5.
+Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, size_t slot_floats) {
+  constexpr int64_t kGrain = 128;
   Plan k{blocks, 1, 0x7fffff00, 16};
-  const int64_t units = (int64_t)blocks * heads;
-  if (units <= 0 || units >= want || units > kTickets || keys <= least) return k;
-  int64_t n = (want + units - 1) / units;
-  if (n > most) n = most;
-  k.bytes = kTickets * 4 + (size_t)units * n * slot_floats * 4;
-  const int64_t each = ((keys + n - 1) / n + least - 1) / least * least;
-  k.slices = (int)((keys + each - 1) / each);
-  k.slice_keys = (int)each;
+  const int64_t units = (int64_t)blocks * heads, slot = (int64_t)slot_floats * 4, bytes_most = (int64_t)60 << 20;
+  if (units <= 0 || units > kTickets || keys <= kGrain) return k;
+  double least = 0;
+  for (int64_t n = 1; n <= kMaxTileSlices && (n == 1 || units * n * slot <= bytes_most); ++n) {
+    const int64_t each = ((keys + n - 1) / n + kGrain - 1) / kGrain * kGrain;
+    if ((keys + each - 1) / each != n) continue;
+    const double a_unit = (double)(full * heads * n) / (double)cus;
+    const double slow = a_unit <= 0.82 ? 1.0 : a_unit <= 1.0 ? 1.25 : a_unit <= 2.0 ? 1.85 : 0.93 * a_unit + 0.4;
+    const double time = slow * (double)((each + 63) / 64 + (n > 1 ? 12 : 5));
+    if (n == 1 || time < 0.95 * least) {
+      least = time;
+      k.slices = (int)n;
+      k.slice_keys = (int)each;
+    }
+  }
+  if (k.slices > 1) k.bytes = kTickets * 4 + (size_t)(units * k.slices * slot);
+  else k.slice_keys = 0x7fffff00;
   return k;
 }
 
@@ -64,7 +78,7 @@ Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int
   }
   if (k.many) {
     const int blocks = (int)(tokens * group / kTileRows) + seqs;
-    k.m = plan(blocks, heads, keys, 2 * cus, kMaxTileSlices, 512, paged_attn_tile_slot_floats(D));
+    k.m = plan_many(blocks, (tokens * group + kTileRows - 1) / kTileRows, heads, keys, cus, paged_attn_tile_slot_floats(D));
   }
   return k;
 }

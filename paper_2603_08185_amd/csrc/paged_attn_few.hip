@@ -377,28 +377,7 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
   join_slices<DT, D, BM, 256>(p, k, h, part.count, [&](int u) { return part.slot(u); }, (float*)lds, tok0, vs, tid);   // (the regions of the waves are free)
 }
 
-// What a lane knows of a sequence: its new tokens, its keys, and the blocks of 64 keys that it gives a key head to do: none if it is not this
-// kernel's, at least one else (its rows have to be written).
-constexpr int kUnit = 64;
-struct Sequence { int c0, n, L, blocks; };
-__device__ __forceinline__ Sequence sequence(const AttnParams& p, int b) {
-  Sequence s{p.c.cu[b], 0, p.c.len[b], 0};
-  s.n = p.c.cu[b + 1] - s.c0;
-  if (takes(p, s.c0, s.n)) {
-    const int end = min(s.L, p.c.width << p.c.page_shift), base = (p.window > 0 ? max(0, s.L - s.n - p.window + 1) : 0) & ~15;
-    s.blocks = end > base ? (end - base - 1) / kUnit + 1 : 1;
-  }
-  return s;
-}
-// sum over the lanes up to each one
-__device__ __forceinline__ int sum_upto(int v, int lane) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);     // 1, 2, 4 and 8 lanes before, within 16
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  const int a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47);
-  return v + (lane >= 48 ? a + b + c : lane >= 32 ? a + b : lane >= 16 ? a : 0);
-}
+constexpr int kUnit = 64;                                     // keys of a piece of a line
 
 template <int DT, bool F8, int D, int NB>
 __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
@@ -406,49 +385,36 @@ __global__ __launch_bounds__(256, 2) void paged_attn_few_kernel(AttnParams p) {
   constexpr int BM = 16 * NB;
   __shared__ __align__(16) char lds[kWaves * S::REGION];
   __shared__ float stat[kWaves][BM][2];
-  const int l = threadIdx.x & 63, heads = p.c.heads;
+  const int heads = p.c.heads;
   // neighbouring workgroups have different key heads
   const int number = uniform(blockIdx.x / heads), h = blockIdx.x - number * heads;
   if (p.slices <= 1) {                                        // nowhere to meet: a workgroup takes a sequence whole
     const int c0 = uniform(p.c.cu[number]), n = uniform(p.c.cu[number + 1]) - c0;
     if (!takes(p, c0, n)) return;
-    const RowBlock k = row_block_at<BM>(p, number, c0, n, uniform(p.c.len[number]), 0);
+    const RowBlock k = row_block<BM>(p, number, c0, n, uniform(p.c.len[number]), 0);
     stretch<DT, F8, D, NB>(p, k, h, k.begin & ~15, max(k.end, 0), false, {}, lds, stat);
     return;
   }
-  // Every wave for itself: a lane counts the blocks of some sequences, and knows what lies before them.
-  const int per = (p.c.seqs + 63) / 64, b0 = l * per;
-  Sequence s{};                                               // the last that the lane looked at
-  int own = 0;
-  for (int i = min(per, p.c.seqs - b0) - 1; i >= 0; --i) {    // (the first one last)
-    s = sequence(p, b0 + i);
-    own += s.blocks;
-  }
-  const int upto = sum_upto(own, l), total = __builtin_amdgcn_readlane(upto, 63);
+  // (a sequence has one piece at least: its rows have to be written)
+  const auto pieces = [&](int c0, int n, int L) {
+    const int end = min(L, p.c.width << p.c.page_shift), base = (p.window > 0 ? max(0, L - n - p.window + 1) : 0) & ~15;
+    return end > base ? (end - base - 1) / kUnit + 1 : 1;
+  };
+  Line line(p, pieces, threadIdx.x & 63);
   // a share: of the head's line, but not too little for a workgroup, nor so little that too many meet
-  const int wanted = gridDim.x / heads;
+  const int wanted = gridDim.x / heads, total = line.total;
   const int share = max(max(p.slice_keys / kUnit, total / (kMaxSlices - 2) + 1), (total + wanted - 1) / wanted);
   int at = (int)min((int64_t)number * share, (int64_t)total);
   const int stop = min(at + share, total);
   while (at < stop) {
-    const int lane = __builtin_ctzll(__ballot(own > 0 && at >= upto - own && at < upto));
-    int b = b0, from = upto - own;
-    if (l == lane && own > s.blocks) {                        // several sequences: which of them
-      s = sequence(p, b);
-      while (at >= from + s.blocks) {
-        from += s.blocks;
-        s = sequence(p, ++b);
-      }
-    }
-    const RowBlock k = row_block_at<BM>(p, __builtin_amdgcn_readlane(b, lane), __builtin_amdgcn_readlane(s.c0, lane),
-                                        __builtin_amdgcn_readlane(s.n, lane), __builtin_amdgcn_readlane(s.L, lane), 0);
-    const int begins = __builtin_amdgcn_readlane(from, lane), ends = begins + __builtin_amdgcn_readlane(s.blocks, lane);
-    const int until = min(stop, ends), base = k.begin & ~15;
-    const bool cut = at > begins || until < ends;
-    const int k0 = base + (at - begins) * kUnit, k1 = until < ends ? base + (until - begins) * kUnit : max(k.end, 0);
+    const Sequence x = line.find(at);
+    const RowBlock k = row_block<BM>(p, x.b, x.c0, x.n, x.L, 0);
+    const int ends = x.before + x.pieces, until = min(stop, ends), base = k.begin & ~15;
+    const bool cut = at > x.before || until < ends;
+    const int k0 = base + (at - x.before) * kUnit, k1 = until < ends ? base + (until - x.before) * kUnit : max(k.end, 0);
     Part<BM * (D + 2)> part{};
     if (cut) {
-      const int first = begins / share;
+      const int first = x.before / share;
       part = {p.part + (int64_t)h * wanted * 2 * (BM * (D + 2)), p.tickets + h * wanted + first, first, number - first, (ends - 1) / share - first + 1};
     }
     stretch<DT, F8, D, NB>(p, k, h, k0, k1, cut, part, lds, stat);

@@ -59,11 +59,16 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(AttnParams 
   const int tid = threadIdx.x, l = tid & 63, w = uniform(tid >> 6);
   const int n32 = l & 31, half = l >> 5;
   const int G = p.group;
-  // the rows that see most keys come last in a sequence and start first; neighbouring workgroups have different key heads
-  const int units = gridDim.x / p.c.heads;
-  const int h = blockIdx.x % p.c.heads, block = units - 1 - blockIdx.x / p.c.heads, s = blockIdx.z;
-  const RowBlock k = row_block<BM>(p, block, l);
-  if (k.rows <= 0) return;
+  // a sequence's pieces of work are blocks of BM rows; those that see most keys come last and start first; neighbouring workgroups have different
+  // key heads
+  const auto pieces = [&](int, int n, int) { return (n * G + BM - 1) / BM; };
+  Line line(p, pieces, l);
+  // (workgroups without work are the last of the grid: between the others they would make two of these meet on a compute unit)
+  const int unit = uniform(blockIdx.x / p.c.heads), h = blockIdx.x - unit * p.c.heads, number = unit / p.slices, s = unit - number * p.slices;
+  if (number >= line.total) return;
+  const int block = line.total - 1 - number;
+  const Sequence seq = line.find(block);
+  const RowBlock k = row_block<BM>(p, seq.b, seq.c0, seq.n, seq.L, (block - seq.before) * BM);
   const int base = k.begin & ~15;
   const int ns = k.end > base ? min((k.end - base - 1) / p.slice_keys + 1, p.slices) : 1;
   if (s >= ns) return;
@@ -360,7 +365,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_attn_tile_kernel(AttnParams 
 
 template <int DT, bool F8, int D>
 int launch(const AttnParams& p, int blocks, hipStream_t st) {
-  hipLaunchKernelGGL((paged_attn_tile_kernel<DT, F8, D, 4>), dim3((unsigned)(blocks * p.c.heads), 1, (unsigned)p.slices), dim3(256), 0, st, p);
+  hipLaunchKernelGGL((paged_attn_tile_kernel<DT, F8, D, 4>), dim3((unsigned)(blocks * p.slices * p.c.heads)), dim3(256), 0, st, p);
   return hipGetLastError() == hipSuccess ? SERQ_OK : SERQ_EHIP;
 }
 
