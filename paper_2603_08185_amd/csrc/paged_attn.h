@@ -196,5 +196,6 @@ int paged_attn_few_resident(int nb, bool f8, int D);          // workgroups that
 int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, int workgroups, hipStream_t st);
 size_t paged_attn_tile_slot_floats(int D);
 int launch_paged_attn_tile(const AttnParams& p, int dtype, bool f8, int D, int blocks, hipStream_t st);
+int launch_paged_attn_mixed(const AttnParams& many, const AttnParams& few, int dtype, bool f8, int D, int blocks, int shares, hipStream_t st);
 
 }  // namespace serq

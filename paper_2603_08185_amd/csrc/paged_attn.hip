@@ -4,10 +4,10 @@
 namespace serq {
 namespace {
 
-constexpr int kTickets = 4096;                                // words at the start of a workspace, whatever the call
+// A workspace: the tickets of the kernel for few rows, those of the kernel for many, whatever the call; then the slots of the first, those of the second.
+constexpr int kTickets = 4096;
+constexpr size_t kTicketBytes = 2 * kTickets * 4;
 
-// Sequences with more rows than this go to the kernel for many.
-constexpr int kFewRows = 32;
 constexpr int kFewKeys = 256;                                 // keys of a share of the kernel for few rows, at least
 
 // (rows fit 31 bits, the threads of a grid 32)
@@ -18,19 +18,21 @@ bool counts_ok(int64_t tokens, int64_t seqs, int q_heads, int heads) {
 // One kernel's share of a call.
 struct Plan {
   int blocks, slices, slice_keys;
-  size_t bytes;
+  size_t bytes;           // of slots
 };
+
+constexpr size_t kManyRoom = 46u << 20;                        // most that its slices take
 
 // The kernel for many rows: blocks of rows times key heads are the workgroups; where they would leave compute units idle, the keys (at most `keys` that
 // a row block sees) are cut into slices.  Taken is the number of slices with the shortest time.  A tile of 64 keys takes a workgroup about 1 us, or
 // 1.85 where two share a compute unit (which they do as soon as there are nearly as many as units); to begin takes 5 tiles' time, to begin
-// and to meet 12.  `blocks` counts a block more for each sequence than may be needed; `full` is what there is at least.
+// and to meet 8 and one a slice.  `blocks` counts a block more for each sequence than may be needed; `full` is what there is at least.
 // Measured (32 query and 8 key heads; us with 1 / 2 / 3 / 4 / 5 / 8 slices): 384 tokens after 3500 66.6 / 43.1 / 44.8 / 45.5 / 45.2 / 48.4, 256 after
 // 8000 131.7 / 75.5 / 56.2 / 62.1 / 61.0 / 60.0, 100 after 30000 469 / 245 / 171 / 134 / 114 / 87, 512 fresh ones 14.9 / 16.9 / 17.3 / 21.5.
-Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, size_t slot_floats) {
+Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, size_t slot_floats, size_t room) {
   constexpr int64_t kGrain = 128;
-  Plan k{blocks, 1, 0x7fffff00, 16};
-  const int64_t units = (int64_t)blocks * heads, slot = (int64_t)slot_floats * 4, bytes_most = (int64_t)60 << 20;
+  Plan k{blocks, 1, 0x7fffff00, 0};
+  const int64_t units = (int64_t)blocks * heads, slot = (int64_t)slot_floats * 4, bytes_most = (int64_t)(room < kManyRoom ? room : kManyRoom);
   if (units <= 0 || units > kTickets || keys <= kGrain) return k;
   double least = 0;
   for (int64_t n = 1; n <= kMaxTileSlices && (n == 1 || units * n * slot <= bytes_most); ++n) {
@@ -38,47 +40,55 @@ Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, s
     if ((keys + each - 1) / each != n) continue;
     const double a_unit = (double)(full * heads * n) / (double)cus;
     const double slow = a_unit <= 0.82 ? 1.0 : a_unit <= 1.0 ? 1.25 : a_unit <= 2.0 ? 1.85 : 0.93 * a_unit + 0.4;
-    const double time = slow * (double)((each + 63) / 64 + (n > 1 ? 12 : 5));
+    const double time = slow * (double)((each + 63) / 64 + (n > 1 ? 8 + n : 5));
     if (n == 1 || time < 0.95 * least) {
       least = time;
       k.slices = (int)n;
       k.slice_keys = (int)each;
     }
   }
-  if (k.slices > 1) k.bytes = kTickets * 4 + (size_t)(units * k.slices * slot);
+  if (k.slices > 1) k.bytes = (size_t)(units * k.slices * slot);
   else k.slice_keys = 0x7fffff00;
   return k;
 }
 
 struct Plans {
   bool few, many;         // which kernels have work
-  int nb;                 // few: blocks of 16 nb rows, one a sequence
+  int few_rows, nb;       // sequences with up to few_rows rows are the first one's where both have; its blocks have 16 nb
   Plan f, m;
 };
 
-Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int heads, int group, int D, bool f8) {
+// room: bytes of the workspace
+Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int heads, int group, int D, bool f8, size_t room) {
   Plans k{};
   if (max_q > tokens) max_q = (int)tokens;
+  if (max_kv > 0x7fffffff) max_kv = 0x7fffffff;
   const int64_t rows = (int64_t)max_q * group;
-  k.many = rows > kFewRows;
+  k.many = rows > 32;
   k.few = !k.many || (seqs > 1 && tokens < (int64_t)max_q * seqs);   // (a sequence alone, or all alike: none is short)
+  // beside a chunk, what is short is a token or a few
+  k.few_rows = k.many && group <= 16 ? 16 : 32;
+  k.nb = rows <= 16 || k.few_rows == 16 ? 1 : 2;
   int64_t keys = max_kv;
   if (window > 0 && keys > (int64_t)window + max_q) keys = (int64_t)window + max_q;
   const int64_t cus = device_cu_count();
+  room = room > kTicketBytes ? room - kTicketBytes : 0;
   if (k.few) {
-    k.nb = rows <= 16 ? 1 : 2;
     // as many workgroups as run together, each with an equal share of a head's keys; many more sequences than that are even enough by themselves
     const int64_t together = cus * paged_attn_few_resident(k.nb, f8, D), whole = (int64_t)seqs * heads;
-    k.f = Plan{(int)whole, 1, 0, 16};
-    if (whole < 16 * together && (together + heads - 1) / heads * heads <= kTickets) {
-      const int64_t most = seqs * ((keys + kFewKeys - 1) / kFewKeys + 1), each = (together + heads - 1) / heads;
-      k.f = Plan{(int)(each < most ? each : most) * heads, 2, kFewKeys, 0};
-      k.f.bytes = kTickets * 4 + (size_t)k.f.blocks * 2 * paged_attn_few_slot_floats(k.nb, D) * 4;
-    }
+    const int64_t slots = 2 * (int64_t)paged_attn_few_slot_floats(k.nb, D) * 4 * heads;   // bytes of a workgroup for each head
+    const int64_t most = seqs * ((keys + kFewKeys - 1) / kFewKeys + 1);
+    int64_t each = (together + heads - 1) / heads;
+    if (each > most) each = most;
+    if (each > (int64_t)room / slots) each = (int64_t)room / slots;
+    if (each > kTickets / heads) each = kTickets / heads;
+    k.f = Plan{(int)whole, 1, 0, 0};
+    if (whole < 16 * together && each > 0) k.f = Plan{(int)each * heads, 2, kFewKeys, (size_t)(each * slots)};
+    room -= k.f.bytes;
   }
   if (k.many) {
     const int blocks = (int)(tokens * group / kTileRows) + seqs;
-    k.m = plan_many(blocks, (tokens * group + kTileRows - 1) / kTileRows, heads, keys, cus, paged_attn_tile_slot_floats(D));
+    k.m = plan_many(blocks, (tokens * group + kTileRows - 1) / kTileRows, heads, keys, cus, paged_attn_tile_slot_floats(D), room);
   }
   return k;
 }
@@ -94,8 +104,8 @@ size_t serq_paged_attn_workspace_bytes(int64_t tokens, int seqs, int max_q, int6
   if (tokens < 0 || tokens > kKvTokens || seqs < 0 || seqs > 65536 || max_q < 0 || max_kv < 0 || kv_heads < 1 || kv_heads > 1024 ||
       q_heads < 1 || q_heads > 65535 || q_heads % kv_heads || (dim != 64 && dim != 128) || !counts_ok(tokens, seqs, q_heads, kv_heads))
     return 0;
-  const Plans k = plans(tokens, seqs, max_q, max_kv, 0, kv_heads, q_heads / kv_heads, dim, false);
-  return k.f.bytes > k.m.bytes ? k.f.bytes : k.m.bytes;       // (the two kernels of a call follow each other)
+  const Plans k = plans(tokens, seqs, max_q, max_kv, 0, kv_heads, q_heads / kv_heads, dim, false, (size_t)1 << 40);
+  return kTicketBytes + k.f.bytes + k.m.bytes;
 }
 
 int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int dtype, const serq_kv_cache* cache,
@@ -116,29 +126,22 @@ int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int d
   p.q = (const char*)q; p.out = (char*)out; p.lse = lse;
   p.ldq = 2 * ldq; p.ldqh = 2 * ldqh; p.ldo = 2 * ldo; p.ldoh = 2 * ldoh;
   p.q_heads = q_heads; p.group = q_heads / cache->heads; p.window = window; p.scale = scale;
-  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, window, cache->heads, p.group, D, cache->dtype == SERQ_F8);
-  const auto place = [&](const Plan& n) {
-    const bool sliced = n.slices > 1 && workspace && workspace_bytes >= n.bytes;
-    p.slices = sliced ? n.slices : 1;
-    p.slice_keys = sliced ? n.slice_keys : 0x7fffff00;
-    p.tickets = (uint32_t*)workspace;
-    p.part = (float*)workspace + kTickets;
-  };
   const bool f8 = cache->dtype == SERQ_F8;
-  if (k.many) {
-    p.rows_from = k.few ? kFewRows + 1 : 0;
-    p.rows_to = 0x7fffffff;
-    place(k.m);
-    rc = launch_paged_attn_tile(p, dtype, f8, D, k.m.blocks, (hipStream_t)stream);
-    if (rc != SERQ_OK) return rc;
-  }
-  if (k.few) {
-    p.rows_from = 0;
-    p.rows_to = k.many ? kFewRows + 1 : 0x7fffffff;
-    place(k.f);
-    rc = launch_paged_attn_few(p, dtype, f8, D, k.nb, p.slices > 1 ? k.f.blocks : p.c.seqs * p.c.heads, (hipStream_t)stream);
-  }
-  return rc;
+  if (!workspace) workspace_bytes = 0;
+  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, window, cache->heads, p.group, D, f8, workspace_bytes);
+  AttnParams few = p, many = p;
+  few.slices = k.f.slices; few.slice_keys = k.f.slice_keys;
+  few.rows_from = 0; few.rows_to = k.many ? k.few_rows + 1 : 0x7fffffff;
+  few.tickets = (uint32_t*)workspace;
+  few.part = (float*)((char*)workspace + kTicketBytes);
+  many.slices = k.m.slices; many.slice_keys = k.m.slice_keys;
+  many.rows_from = k.few ? k.few_rows + 1 : 0; many.rows_to = 0x7fffffff;
+  many.tickets = few.tickets + kTickets;
+  many.part = (float*)((char*)workspace + kTicketBytes + k.f.bytes);
+  hipStream_t st = (hipStream_t)stream;
+  if (k.few && k.many && k.nb == 1) return launch_paged_attn_mixed(many, few, dtype, f8, D, k.m.blocks, k.f.blocks, st);
+  if (k.many && (rc = launch_paged_attn_tile(many, dtype, f8, D, k.m.blocks, st)) != SERQ_OK) return rc;
+  return k.few ? launch_paged_attn_few(few, dtype, f8, D, k.nb, k.f.blocks, st) : SERQ_OK;
 }
 
 }  // extern "C"
