@@ -24,11 +24,11 @@ struct Plan {
 constexpr size_t kManyRoom = 46u << 20;                        // most that its slices take
 
 // The kernel for many rows: blocks of rows times key heads are the workgroups; where they would leave compute units idle, the keys (at most `keys` that
-// a row block sees) are cut into slices.  Taken is the number of slices with the shortest time.  A tile of 64 keys takes a workgroup about 1 us, or
-// 1.85 where two share a compute unit (which they do as soon as there are nearly as many as units); to begin takes 5 tiles' time, to begin
-// and to meet 8 and one a slice.  `blocks` counts a block more for each sequence than may be needed; `full` is what there is at least.
-// Measured (32 query and 8 key heads; us with 1 / 2 / 3 / 4 / 5 / 8 slices): 384 tokens after 3500 66.6 / 43.1 / 44.8 / 45.5 / 45.2 / 48.4, 256 after
-// 8000 131.7 / 75.5 / 56.2 / 62.1 / 61.0 / 60.0, 100 after 30000 469 / 245 / 171 / 134 / 114 / 87, 512 fresh ones 14.9 / 16.9 / 17.3 / 21.5.
+// a row block sees) are cut into slices.  Taken is the number of slices with the shortest time.  A tile of 64 keys takes a workgroup 1.08 us on a
+// compute unit of its own, 1.85 beside another; to begin takes 5 us, to begin and to meet 8 and one a slice.  `blocks` counts a block more for each
+// sequence than may be needed (every sequence's last one is half empty on average); `full` is about what there is.
+// Measured (32 query and 8 key heads; us with 1 / 2 / 3 / 4 / 5 / 8 slices): 384 tokens after 3500 66.6 / 43.1 / 44.8 / 45.5 / 45.2 / 48.4, 100 after 30000
+// 469 / 245 / 171 / 134 / 114 / 87, 512 fresh ones 14.9 / 16.9 / 17.3 / 21.5; 512 after 32000 with 2 / 4 292 / 272, 256 after 8000 with 3 / 4 56.5 / 50.6.
 Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, size_t slot_floats, size_t room) {
   constexpr int64_t kGrain = 128;
   Plan k{blocks, 1, 0x7fffff00, 0};
@@ -39,7 +39,7 @@ Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, s
     const int64_t each = ((keys + n - 1) / n + kGrain - 1) / kGrain * kGrain;
     if ((keys + each - 1) / each != n) continue;
     const double a_unit = (double)(full * heads * n) / (double)cus;
-    const double slow = a_unit <= 0.82 ? 1.0 : a_unit <= 1.0 ? 1.25 : a_unit <= 2.0 ? 1.85 : 0.93 * a_unit + 0.4;
+    const double slow = a_unit <= 1.0 ? 1.08 : a_unit <= 2.0 ? 1.85 : 0.93 * a_unit + 0.4;
     const double time = slow * (double)((each + 63) / 64 + (n > 1 ? 8 + n : 5));
     if (n == 1 || time < 0.95 * least) {
       least = time;
@@ -88,7 +88,9 @@ Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int
   }
   if (k.many) {
     const int blocks = (int)(tokens * group / kTileRows) + seqs;
-    k.m = plan_many(blocks, (tokens * group + kTileRows - 1) / kTileRows, heads, keys, cus, paged_attn_tile_slot_floats(D), room);
+    // (sequences of about the longest one's length, and half of the last block of each)
+    const int64_t alike = 2 * tokens / max_q < seqs ? 2 * tokens / max_q : seqs;
+    k.m = plan_many(blocks, (tokens * group + kTileRows - 1) / kTileRows + (alike - 1) / 2, heads, keys, cus, paged_attn_tile_slot_floats(D), room);
   }
   return k;
 }
