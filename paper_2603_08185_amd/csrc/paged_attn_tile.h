@@ -197,6 +197,15 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
   };
   constexpr int QK = 2 * STEPS, AHEAD = 4;                    // products of a tile's scores; operands of K that are under way
   // One tile: its scores `sc` become weights and meet V, while the next tile's scores are computed (MORE).  K runs a tile ahead of V.
+  float top;                                                  // largest of the lane's scores of the tile whose turn it is
+  const auto largest = [](const v16f (&sc)[2]) {
+    float x = sc[0][0];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x = fmaxf(x, sc[kb][e]);
+    return x;
+  };
   auto step = [&](int t, v16f (&sc)[2], v16f (&next)[2], auto more) {
     constexpr bool MORE = decltype(more)::value;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -228,12 +237,8 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
           const int j = 32 * kb + 8 * (e / 4) + e % 4;
           if (j < from || j >= to) sc[kb][e] = -INFINITY;
         }
+      top = largest(sc);
     }
-    float top = sc[0][0];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[kb][e]);
     if (__ballot(top > ref + slack)) {
       const uint32_t bits = __float_as_uint(top);
       const auto two = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
@@ -276,6 +281,13 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
       for (int d = 0; d < DB; ++d) {
         o[d] = mfma<DT>(vf[g & 1][d], pw[g], o[d]);
         if (g < 3) vf[(g + 1) & 1][d] = v_piece(t, g + 1, d);
+        if constexpr (MORE) {                                 // the next tile's largest score, some of them a time
+          const int n = g * DB + d;
+          if (n == 0) top = next[0][0];
+#pragma unroll
+          for (int e = n * 32 / (4 * DB); e < (n + 1) * 32 / (4 * DB); ++e) top = fmaxf(top, next[e / 16][e % 16]);
+          asm volatile("" : "+v"(top));
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     if (more_k) commit_k(t + 2);
@@ -300,6 +312,7 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
       for (int e = 0; e < 16; ++e) sa[kb][e] = 0.0f;
 #pragma unroll
     for (int i = 0; i < QK; ++i) sa[i / STEPS] = mfma<DT>(k_piece(0, i), q[i % STEPS], sa[i / STEPS]);
+    top = largest(sa);
     int t = 0;
     for (; t + 2 < nt; t += 2) {
       step(t, sa, sb, std::true_type{});
