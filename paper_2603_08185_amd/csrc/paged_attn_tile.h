@@ -195,7 +195,7 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
     const u2 y = lds_column4(at), z = lds_column4(at + 8 * ROW);
     return (u4){y.x, y.y, z.x, z.y};
   };
-  constexpr int QK = 2 * STEPS, AHEAD = 4;                    // products of a tile's scores; operands of K that are under way
+  constexpr int QK = 2 * STEPS, AHEAD = 2;                    // products of a tile's scores; operands of K that are under way
   // One tile: its scores `sc` become weights and meet V, while the next tile's scores are computed (MORE).  K runs a tile ahead of V.
   float top;                                                  // largest of the lane's scores of the tile whose turn it is
   const auto largest = [](const v16f (&sc)[2]) {
@@ -258,6 +258,8 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; ++e) next[kb][e] = 0.0f;
+    // (the wave that is here goes before the other one of the SIMD, which is most often at its products with V: see the figures above)
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int i = 0; i < QK; ++i) {
       if constexpr (MORE) {
@@ -275,6 +277,7 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
       asm volatile("" : "+v"(sum), "+v"(sum2));               // (else the additions are put off, and their operands kept)
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
 #pragma unroll
     for (int g = 0; g < 4; ++g)
 #pragma unroll
