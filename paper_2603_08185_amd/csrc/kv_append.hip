@@ -42,15 +42,57 @@ __device__ __forceinline__ void turn(float& x, float& y, float c, float s) {
   y = yc + xs;
 }
 
-// One token a workgroup, one pair of pieces a thread (more where a token has more pairs than threads).
+// One token a workgroup, one pair of pieces a thread (more where a token has more pairs than threads).  What does not hang on the token's place is
+// asked for before that is known: the token's values with the ends and lengths of the sequences, then the page with the rotation.
 template <int DT, bool F8, int D, bool INTER>
 __global__ __launch_bounds__(512) void kv_append_kernel(AppendParams p) {
   constexpr int PP = D / 16;                                  // pairs of a head
-  const int t = blockIdx.x;
-  const int lane = threadIdx.x & 63;
-  const int b = sequences_before(t, p.c.seqs, lane, [&](int i) { return p.c.cu[i + 1]; });
-  if (b >= p.c.seqs) return;                                  // a row of no sequence
-  const int pos = p.c.len[b] - p.c.cu[b + 1] + t;
+  const int t = blockIdx.x, lane = threadIdx.x & 63;
+
+  struct Item {
+    int h, d0, d1;                                            // head of its kind, first channels of the two pieces
+    bool is_q, is_k, rotated;
+    Raw8<DT> x, y;
+  };
+  const auto fetch = [&](int it) {
+    Item m;
+    const int head = it / PP, j = it % PP;
+    m.is_q = head < p.q_heads;
+    m.is_k = !m.is_q && head < p.q_heads + p.c.heads;
+    m.h = m.is_q ? head : m.is_k ? head - p.q_heads : head - p.q_heads - p.c.heads;
+    m.rotated = (m.is_q || m.is_k) && j < p.rot / 16;
+    const bool split = m.rotated && !INTER;                   // the two pieces lie rot / 2 channels apart
+    m.d0 = split ? 8 * j : 16 * j;
+    m.d1 = split ? m.d0 + p.rot / 2 : m.d0 + 8;
+    const char* src = m.is_q ? p.q + t * p.ldq + m.h * p.ldqh : m.is_k ? p.k + t * p.ldk + m.h * p.ldkh : p.v + t * p.ldv + m.h * p.ldvh;
+    m.x.a = *(const u4*)(src + 2 * m.d0);
+    m.y.a = *(const u4*)(src + 2 * m.d1);
+    return m;
+  };
+  // (the sequences first: loads come back in their order)
+  const auto ask = [&](int b, int& end, int& len) {
+    const int i = min(b + lane, p.c.seqs - 1);
+    end = p.c.cu[i + 1];
+    len = p.c.len[i];
+  };
+  int b = 0, pos, end, len;
+  ask(0, end, len);
+  int it = threadIdx.x;
+  Item m{};
+  if (it < p.items) m = fetch(it);
+  __builtin_amdgcn_sched_barrier(0);
+
+  // the token's sequence: the first that ends behind it
+  for (;;) {
+    const int c = __builtin_popcountll(__ballot(b + lane < p.c.seqs && end <= t));
+    b += c;
+    if (b >= p.c.seqs) return;                                // a row of no sequence
+    if (c < 64) {
+      pos = __builtin_amdgcn_readlane(len, c) - __builtin_amdgcn_readlane(end, c) + t;
+      break;
+    }
+    ask(b, end, len);
+  }
   const int turned = min(max(p.positions ? p.positions[t] : pos, 0), p.rows - 1);
   const int slot = pos >> p.c.page_shift;                     // (negative for a negative position)
   int page = -1;
@@ -58,25 +100,19 @@ __global__ __launch_bounds__(512) void kv_append_kernel(AppendParams p) {
   if (page >= p.c.pages) page = -1;
   const int row = pos & ((1 << p.c.page_shift) - 1);
 
-  for (int it = threadIdx.x; it < p.items; it += blockDim.x) {
-    const int head = it / PP, j = it % PP;
-    const bool is_q = head < p.q_heads, is_k = !is_q && head < p.q_heads + p.c.heads;
-    const int h = is_q ? head : is_k ? head - p.q_heads : head - p.q_heads - p.c.heads;
-    const bool rotated = (is_q || is_k) && j < p.rot / 16;
-    const bool split = rotated && !INTER;                     // the two pieces lie rot / 2 channels apart
-    const int d0 = split ? 8 * j : 16 * j, d1 = split ? d0 + p.rot / 2 : d0 + 8;
-    const char* src = is_q ? p.q + t * p.ldq + h * p.ldqh : is_k ? p.k + t * p.ldk + h * p.ldkh : p.v + t * p.ldv + h * p.ldvh;
-    Raw8<DT> x, y;
-    x.a = *(const u4*)(src + 2 * d0);
-    y.a = *(const u4*)(src + 2 * d1);
+  for (; it < p.items;) {
     float a[8], e[8];
-    values8<DT>(x, a);
-    values8<DT>(y, e);
-    if (rotated) {
-      const int64_t at = (int64_t)turned * (p.rot / 2) + 8 * j;
+    values8<DT>(m.x, a);
+    values8<DT>(m.y, e);
+    if (m.rotated) {
+      const int64_t at = (int64_t)turned * (p.rot / 2) + (INTER ? m.d0 / 2 : m.d0);
       float c[8], s[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { c[i] = p.cos[at + i]; s[i] = p.sin[at + i]; }
+      for (int i = 0; i < 2; ++i) {
+        const v4f cc = *(const v4f*)(p.cos + at + 4 * i), ss = *(const v4f*)(p.sin + at + 4 * i);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) { c[4 * i + n] = cc[n]; s[4 * i + n] = ss[n]; }
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         if constexpr (INTER) {                                // pairs (0,1) .. (6,7) of the first piece, then of the second
@@ -87,23 +123,25 @@ __global__ __launch_bounds__(512) void kv_append_kernel(AppendParams p) {
         }
       }
     }
-    if (is_q) {
-      char* dst = p.qo + t * p.ldqo + h * p.ldqoh;
-      *(u4*)(dst + 2 * d0) = to16<DT>(a);
-      *(u4*)(dst + 2 * d1) = to16<DT>(e);
+    if (m.is_q) {
+      char* dst = p.qo + t * p.ldqo + m.h * p.ldqoh;
+      *(u4*)(dst + 2 * m.d0) = to16<DT>(a);
+      *(u4*)(dst + 2 * m.d1) = to16<DT>(e);
     } else if (page >= 0) {
-      char* dst = is_k ? p.c.k + page * p.c.k_page + row * p.c.k_token + h * p.c.k_head
-                       : p.c.v + page * p.c.v_page + row * p.c.v_token + h * p.c.v_head;
+      char* dst = m.is_k ? p.c.k + page * p.c.k_page + row * p.c.k_token + m.h * p.c.k_head
+                         : p.c.v + page * p.c.v_page + row * p.c.v_token + m.h * p.c.v_head;
       if constexpr (F8) {
-        const float* sc = is_k ? p.c.k_scale : p.c.v_scale;
-        const float scale = sc ? sc[h] : 1.0f;
-        *(u2*)(dst + d0) = to_e4m3(a, scale);
-        *(u2*)(dst + d1) = to_e4m3(e, scale);
+        const float* sc = m.is_k ? p.c.k_scale : p.c.v_scale;
+        const float scale = sc ? sc[m.h] : 1.0f;
+        *(u2*)(dst + m.d0) = to_e4m3(a, scale);
+        *(u2*)(dst + m.d1) = to_e4m3(e, scale);
       } else {
-        *(u4*)(dst + 2 * d0) = to16<DT>(a);
-        *(u4*)(dst + 2 * d1) = to16<DT>(e);
+        *(u4*)(dst + 2 * m.d0) = to16<DT>(a);
+        *(u4*)(dst + 2 * m.d1) = to16<DT>(e);
       }
     }
+    it += blockDim.x;
+    if (it < p.items) m = fetch(it);
   }
 }
 
