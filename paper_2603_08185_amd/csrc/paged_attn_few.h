@@ -53,6 +53,45 @@ template <int DT, int D, int BM, int THREADS, class Slot>
 __device__ __forceinline__ void join_slices(const AttnParams& p, const RowBlock& k, int h, int ns, const Slot& slot, float* scratch, int tok0,
                                             float vs, int tid) {
   const int l = tid & 63, w = uniform(tid >> 6);
+  const auto put = [&](int r, int d, const v2f& acc, float f) {
+    const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
+    char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (int64_t)(h * p.group + g) * p.ldoh;
+    *(uint32_t*)(dst + 2 * d) = pack16<DT>(acc[0] * f, acc[1] * f);
+  };
+  const auto put_lse = [&](int r, float m, float sum) {
+    const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
+    if (p.lse) p.lse[(int64_t)(tok0 + i) * p.q_heads + h * p.group + g] = row_lse(m, sum);
+  };
+  // A load takes a microsecond here, so as many as can be are under way together.  Few slices: every thread computes their weights by itself
+  // (past the end: the last slot again, without weight).
+  const auto alone = [&](auto number) {
+    constexpr int N = decltype(number)::value;
+    for (int it = tid; it < k.rows * (D / 2); it += THREADS) {
+      const int r = it / (D / 2), d = 2 * (it % (D / 2));
+      v2f st[N], x[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float* from = slot(min(e, ns - 1));
+        st[e] = get2(from + BM * D + 2 * r);
+        x[e] = get2(from + r * D + d);
+      }
+      float top = st[0][0], all = 0.0f;
+#pragma unroll
+      for (int e = 1; e < N; ++e) top = fmaxf(top, st[e][0]);
+      v2f acc = {0.0f, 0.0f};
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e < ns) {
+          const float f = exp2_fast(st[e][0] - top);
+          all += f * st[e][1];
+          acc += f * x[e];
+        }
+      put(r, d, acc, row_factor(all, vs));
+      if (d == 0) put_lse(r, top, all);
+    }
+  };
+  if (ns <= 4) return alone(std::integral_constant<int, 4>{});
+  if (ns <= 12) return alone(std::integral_constant<int, 12>{});
   float* weight = scratch + BM;                               // [rows][ns]: each slice's weight; scratch[row]: what the row is multiplied by
   for (int r = w; r < k.rows; r += THREADS / 64) {
     float m[(kMaxSlices + 63) / 64], n[(kMaxSlices + 63) / 64], top = -FLT_MAX;
@@ -82,29 +121,22 @@ __device__ __forceinline__ void join_slices(const AttnParams& p, const RowBlock&
     all = wave_reduce(all, [](float x, float y) { return x + y; });
     if (l == 0) {
       scratch[r] = row_factor(all, vs);
-      const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
-      if (p.lse) p.lse[(int64_t)(tok0 + i) * p.q_heads + h * p.group + g] = row_lse(top, all);
+      put_lse(r, top, all);
     }
   }
   __syncthreads();
   for (int it = tid; it < k.rows * (D / 2); it += THREADS) {
     const int r = it / (D / 2), d = 2 * (it % (D / 2));
     v2f acc = {0.0f, 0.0f};
-    // N loads under way together: a load takes a microsecond here (past the end: the last slot again, without weight)
-    const auto some = [&](int u, auto number) {
-      constexpr int N = decltype(number)::value;
-      v2f x[N];
+    for (int u = 0; u < ns; u += 16) {
+      v2f x[16];
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[e] = get2(slot(min(u + e, ns - 1)) + r * D + d);
+      for (int e = 0; e < 16; ++e) x[e] = get2(slot(min(u + e, ns - 1)) + r * D + d);
 #pragma unroll
-      for (int e = 0; e < N; ++e) acc += (u + e < ns ? weight[r * ns + min(u + e, ns - 1)] : 0.0f) * x[e];
-    };
-    if (ns <= 8) some(0, std::integral_constant<int, 8>{});
-    else for (int u = 0; u < ns; u += 16) some(u, std::integral_constant<int, 16>{});
-    const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
-    const float f = scratch[r];
-    char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (int64_t)(h * p.group + g) * p.ldoh;
-    *(uint32_t*)(dst + 2 * d) = pack16<DT>(acc[0] * f, acc[1] * f);
+      for (int e = 0; e < 16; ++e)
+        if (u + e < ns) acc += weight[r * ns + u + e] * x[e];
+    }
+    put(r, d, acc, scratch[r]);
   }
 }
 
@@ -127,6 +159,17 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
   asm volatile("" : "+v"(tid));                               // (else what follows from it is kept from stretch to stretch: 67 registers)
   const int l = tid & 63, w = uniform(tid >> 6);
   const int n16 = l & 15, quad = l >> 4, G = p.group, tok0 = k.tok0;
+
+  const int mask = (1 << p.c.page_shift) - 1;
+  const int32_t* table = p.c.table + k.b * p.c.table_ld;
+  const int nt = k1 > k0 ? (k1 - k0 + KEYS - 1) / KEYS : 0;   // tiles of the slice
+  const int mine = nt > w ? (nt - w + kWaves - 1) / kWaves : 0;
+  // the pages of the first tiles (loads come back in their order: these before the queries)
+  const auto key_of = [&](int t) { return k0 + (w + kWaves * (t + l / TG)) * KEYS + 16 * (l % TG); };
+  const auto page_of = [&](int key) { return table[min(key, k.end - 1) >> p.c.page_shift]; };   // (past the end: the last key's)
+  int page = 0;
+  if (mine > 0) page = page_of(key_of(0));
+  __builtin_amdgcn_sched_barrier(0);
 
   // the rows' queries, and the keys that each sees: lo <= j < hi
   u4 q[NB][S::STEPS];
@@ -152,8 +195,6 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
   const float ks = p.c.k_scale ? p.c.k_scale[h] : 1.0f, vs = p.c.v_scale ? p.c.v_scale[h] : 1.0f;
   const float c = p.scale * ks * kLog2e, slack = score_slack(c);
 
-  const int mask = (1 << p.c.page_shift) - 1;
-  const int32_t* table = p.c.table + k.b * p.c.table_ld;
   const char* kbase = p.c.k + h * p.c.k_head;
   const char* vbase = p.c.v + h * p.c.v_head;
   const uint32_t klane = (uint32_t)(n16 * (int)p.c.k_token + quad * 16);
@@ -161,14 +202,11 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
 #pragma unroll
   for (int i = 0; i < KL; ++i) vlane[i] = (uint32_t)((i * S::RPI + l / S::LPR) * (int)p.c.v_token + (l % S::LPR) * 16);
 
-  const int nt = k1 > k0 ? (k1 - k0 + KEYS - 1) / KEYS : 0;   // tiles of the slice
-  const int mine = nt > w ? (nt - w + kWaves - 1) / kWaves : 0;
   // lane: where group lane % TG of the wave's tile lane / TG of the next 64 / TG begins, so that a tile's loads need no arithmetic of their own
-  // (past the end: in the last key's page)
   uint64_t kfrom = 0, vfrom = 0;
-  auto look_up = [&](int t) {
-    const int key = k0 + (w + kWaves * (t + l / TG)) * KEYS + 16 * (l % TG);
-    const int page = min(max(table[min(key, k.end - 1) >> p.c.page_shift], 0), p.c.pages - 1);
+  auto look_up = [&](int t, int page) {
+    const int key = key_of(t);
+    page = min(max(page, 0), p.c.pages - 1);
     kfrom = (uint64_t)(kbase + page * p.c.k_page + (key & mask) * p.c.k_token);
     vfrom = (uint64_t)(vbase + page * p.c.v_page + (key & mask) * p.c.v_token);
   };
@@ -222,7 +260,7 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
   const int cturn = turned<D>(crow) << 4;
 
   if (mine > 0) {
-    look_up(0);
+    look_up(0, page);
     load_k(0);
     load_v(0);
   }
@@ -249,7 +287,7 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
       }
     }
     if constexpr (MORE) {
-      if (((t + 1) * TG & 63) == 0) look_up(t + 1);
+      if (((t + 1) * TG & 63) == 0) look_up(t + 1, page_of(key_of(t + 1)));
       load_k(t + 1);
     }
     __builtin_amdgcn_sched_barrier(0);
