@@ -77,10 +77,10 @@ int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_heads,
  * Attention over the cache: query head h reads key head h / (q_heads / cache->heads),
  *   s_j = scale * q[t,h,:] . K_j,   out[t,h,:] = sum_j softmax(s)_j V_j,   lse[t,h] = log sum_j exp(s_j),
  * over the positions j with 0 <= j <= p and, where window > 0, j > p - window.  A row that sees no key (p < 0) gives out = 0,
- * lse = -inf.  Nothing that lies in the cache outside the positions that the call's tokens of a sequence see reaches a result, whatever it
- * holds, and pages that hold none of them are not read; their table entries may be anything.  Page numbers outside
- * 0 .. pages-1 are clamped, lengths past table_width * page_size cut (nothing is read out of bounds; the result is then
- * meaningless).
+ * lse = -inf.  What a row does not see does not reach its result, whatever it holds, NaN and infinities among it; pages that hold no
+ * position that a token of the call sees are not read, and their table entries may be anything.  (NaN or infinite values that a row does see
+ * make its result NaN or infinite, which of the two is not defined.)  Page numbers outside 0 .. pages-1 are clamped, lengths past
+ * table_width * page_size cut (nothing is read out of bounds; the result is then meaningless).
  *   q, out [tokens, q_heads, dim] in dtype (SERQ_F16 / SERQ_BF16), strides as above; q_heads a multiple of cache->heads.  tokens * q_heads is
  *          at most 2^30, seqs * cache->heads 2^22.
  *   scale  positive and finite.

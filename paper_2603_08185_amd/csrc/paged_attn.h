@@ -26,6 +26,7 @@ struct RowBlock {
   int b, tok0, r0, n, L;  // sequence, its first row of q, the block's first row, new tokens, keys
   int rows;               // rows of the block (<= 0: none)
   int begin, end;         // keys that any of its rows sees: begin <= j < end
+  int all_from, all_to;   // keys that all of its rows see
 };
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 // The block of BM rows from r0 on of sequence b, whose new tokens are rows c0 .. c0+n-1 of q and which has L keys.
@@ -42,6 +43,8 @@ __device__ __forceinline__ RowBlock row_block(const AttnParams& p, int b, int c0
   const int first = L - n + r0 / G, last = L - n + (r0 + k.rows - 1) / G;
   k.end = min(last + 1, p.c.width << p.c.page_shift);
   k.begin = p.window > 0 ? max(0, first - p.window + 1) : 0;
+  k.all_from = p.window > 0 ? max(0, last - p.window + 1) : 0;
+  k.all_to = min(first + 1, k.end);
   return k;
 }
 // whether a sequence is this kernel's (and one that can be)
@@ -150,6 +153,30 @@ __device__ __forceinline__ void widen_e4m3(const u4& w, u4& lo, u4& hi) {
 typedef short v4s __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ u2 lds_column4(const char* p) {
   return __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p));
+}
+
+// Values of keys that some rows of a block see and others do not.  A weight of zero does not make NaN or infinity zero, so in the tiles that hold such keys
+// what is not finite is taken out before the products, and added at the end for the rows that do see it.
+template <int DT>
+__device__ __forceinline__ u4 take_out(u4 x, bool& odd) {
+  constexpr uint32_t M = DT == SERQ_BF16 ? 0x7f80u : 0x7c00u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool a = (x[i] & M) == M, b = (x[i] & (M << 16)) == (M << 16);
+    odd |= a || b;
+    x[i] = (a ? 0u : x[i] & 0xffffu) | (b ? 0u : x[i] & 0xffff0000u);
+  }
+  return x;
+}
+// What was taken out of channel d of key j of sequence b, 0 if nothing was.
+template <int DT, bool F8>
+__device__ __forceinline__ float taken_out(const AttnParams& p, int b, int h, int j, int d) {
+  const int page = min(max(p.c.table[b * p.c.table_ld + (j >> p.c.page_shift)], 0), p.c.pages - 1);
+  const char* row = p.c.v + h * p.c.v_head + page * p.c.v_page + (j & ((1 << p.c.page_shift) - 1)) * p.c.v_token;
+  float v;
+  if constexpr (F8) v = __builtin_amdgcn_cvt_f32_fp8((int)(uint8_t)row[d], 0);
+  else v = Elem<DT>::ld(row, d);
+  return __builtin_isfinite(v) ? 0.0f : v;
 }
 
 template <int DT>

@@ -189,9 +189,7 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
       q[nb][st] = live ? *(const u4*)(src + 2 * at) : (u4){0, 0, 0, 0};
     }
   }
-  // keys that all rows see: no mask there
-  const int all_lo = p.window > 0 ? max(0, k.L - k.n + (k.r0 + k.rows - 1) / G - p.window + 1) : 0;
-  const int all_hi = min(k.L - k.n + k.r0 / G + 1, k.end);
+  const int all_lo = k.all_from, all_hi = k.all_to;           // no mask there
   const float ks = p.c.k_scale ? p.c.k_scale[h] : 1.0f, vs = p.c.v_scale ? p.c.v_scale[h] : 1.0f;
   const float c = p.scale * ks * kLog2e, slack = score_slack(c);
 
@@ -264,6 +262,7 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
     load_k(0);
     load_v(0);
   }
+  bool odd = false;                                           // the lane took something out
   // One tile.  The loads of the next one are sent without a condition (the waits count loads: one that may not have been sent counts as none,
   // and the wait for K would be one for V too), so the last tile is a case of its own.
   const auto tile = [&](int t, auto more) {
@@ -293,6 +292,7 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
     __builtin_amdgcn_sched_barrier(0);
     // V to LDS; rows that no row sees are zero there (a weight of zero does not make NaN zero)
     const bool ends = key0 < k.begin || key0 + KEYS > k.end;
+    const bool partly = (key0 + KEYS > all_hi && key0 < k.end && all_hi < k.end) || (key0 < all_lo && key0 + KEYS > k.begin && k.begin < all_lo);
     int to = vrow * D * 2, turn = cturn;
     asm volatile("" : "+v"(to), "+v"(turn));                   // (else sixteen places in LDS are kept from tile to tile)
 #pragma unroll
@@ -304,10 +304,15 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
       if constexpr (F8) {
         u4 a, b;
         widen_e4m3<DT>(x, a, b);
+        if (partly && (key0 + row < all_lo || key0 + row >= all_hi)) {
+          a = take_out<DT>(a, odd);
+          b = take_out<DT>(b, odd);
+        }
         at += ((2 * vpiece) ^ turned<D>(row)) << 4;
         *(u4*)at = a;
         *(u4*)(at + 16) = b;
       } else {
+        if (partly && (key0 + row < all_lo || key0 + row >= all_hi)) x = take_out<DT>(x, odd);
         *(u4*)(at + ((vpiece ^ turned<D>(row)) << 4)) = x;
       }
     }
@@ -370,6 +375,19 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
   for (int t = 0; t < mine - 1; ++t) tile(t, std::true_type{});
   if (mine > 0) tile(mine - 1, std::false_type{});
 
+  if (__ballot(odd)) {
+    for (int j = max(k0, k.begin); j < min(k1, k.end); ++j) {
+      if (j >= all_lo && j < all_hi) j = all_hi;              // (what all rows see went through the products)
+      if (j >= min(k1, k.end)) break;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+        if (j >= lo[nb] && j < hi[nb])
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[nb][d][e] += taken_out<DT, F8>(p, k.b, h, j, 16 * d + 4 * quad + e);
+    }
+  }
   // the waves meet
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {

@@ -197,6 +197,8 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
   };
   constexpr int QK = 2 * STEPS, AHEAD = 2;                    // products of a tile's scores; operands of K that are under way
   // One tile: its scores `sc` become weights and meet V, while the next tile's scores are computed (MORE).  K runs a tile ahead of V.
+  __shared__ int odd;                                         // something was taken out
+  if (tid == 0) odd = 0;
   float top;                                                  // largest of the lane's scores of the tile whose turn it is
   const auto largest = [](const v16f (&sc)[2]) {
     float x = sc[0][0];
@@ -211,12 +213,16 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();                                          // K of t + 1 and V of t are there; nobody needs K of t or V of t - 1 any more
     const int key0 = k0 + t * kKeys;
-    if (key0 < k.begin || key0 + kKeys > k.end) {
-      // values of keys that no row sees become zero (a weight of zero does not make NaN zero)
+    if (key0 < k.begin || key0 + kKeys > k.end || key0 < k.all_from || key0 + kKeys > k.all_to) {
+      // values of keys that no row sees become zero (a weight of zero does not make NaN zero); of those that some see, what is not finite
+      bool found = false;
       for (int at = tid; at < TILE / 16; at += 64 * NW) {
         const int key = key0 + at / (ROW / 16);
-        if (key < k.begin || key >= k.end) *(u4*)(lds[t & 1][1] + at * 16) = (u4){0, 0, 0, 0};
+        u4* v = (u4*)(lds[t & 1][1] + at * 16);
+        if (key < k.begin || key >= k.end) *v = (u4){0, 0, 0, 0};
+        else if (key < k.all_from || key >= k.all_to) *v = take_out<DT>(*v, found);
       }
+      if (found) odd = 1;
       __syncthreads();
     }
     const bool more_k = t + 2 < nt;
@@ -329,6 +335,18 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
     }
   }
 
+  __syncthreads();
+  if (odd) {
+    for (int j = max(k0, k.begin); j < min(k1, k.end); ++j) {
+      if (j >= k.all_from && j < k.all_to) j = k.all_to;      // (what all rows see went through the products)
+      if (j >= min(k1, k.end)) break;
+      if (j >= lo && j < hi)
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[d][e] += taken_out<DT, F8>(p, k.b, h, j, 32 * d + 8 * (e / 4) + 4 * half + e % 4);
+    }
+  }
   const uint32_t sbits = __float_as_uint(sum + sum2);
   const auto both = __builtin_amdgcn_permlane32_swap(sbits, sbits, false, false);
   float all = __uint_as_float(both[0]) + __uint_as_float(both[1]);

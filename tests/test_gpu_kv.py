@@ -184,6 +184,43 @@ def test_attention_scales(name, scale, gain):
     check_attention(B, out, lse, scale, what=f"{name}, scale {scale}, gain {gain}")
 
 
+@pytest.mark.parametrize("name", ["few", "chunk", "prompt", "ones"])
+@pytest.mark.parametrize("window", [0, 20])
+@pytest.mark.parametrize("dt,fp8", [(torch.bfloat16, False), (torch.float16, False), (torch.bfloat16, True)])
+def test_attention_nan_and_infinity_where_a_row_does_not_look(name, window, dt, fp8):
+    """Single keys and values of the new tokens, and of keys just inside the first window, that are NaN or infinite: rows that do not see them
+    keep their results, rows that see a value like that lose them."""
+    r = np.random.RandomState(3)
+    B = Batch(SETS[name], 4, 2, 128, 16, dt, fp8, "nhd", window=window, seed=13).fill()
+    want = B._attention64(128 ** -0.5)[0]
+    hit = np.zeros(B.T, bool)
+    for b, (n, L) in enumerate(B.seqs):
+        if n < 2:
+            continue
+        lo = B.first[b]
+        spots = {L - 1, max(L - n + n // 2, lo), *( [lo] if window and lo > 0 else [])}
+        for i, j in enumerate(sorted(spots)):
+            page, row = int(B.table[b, j // 16]), j % 16
+            d = int(r.randint(0, 128))
+            v = float("nan") if fp8 or i % 2 == 0 else (float("inf") if i % 4 == 1 else -float("inf"))
+            if fp8:
+                B.V.view(torch.uint8)[page, row, :, d] = 0x7f
+            else:
+                B.V[page, row, :, d] = v
+            if i % 2 == 1 and not fp8:
+                B.K[page, row, :, (d + 1) % 128] = float("nan")
+            t = np.arange(n)
+            sees = (L - n + t >= j) & (True if not window else L - n + t - window < j)
+            hit[B.cu[b]:B.cu[b + 1]] |= sees
+    ws = serq.paged_attention_workspace(B.T, len(B.seqs), B.max_q, B.max_kv, 4, 2, 128, DEV)
+    u = 2.0 ** -8 if dt == torch.bfloat16 else 2.0 ** -11
+    for use in (None, ws):
+        out = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, window=window, k_scale=B.k_scale, v_scale=B.v_scale, ws=use).double().cpu().numpy()
+        fine = np.isfinite(out).all((1, 2))
+        assert np.array_equal(fine, ~hit), f"rows {np.argwhere(fine == hit).ravel()[:10]}"
+        assert np.abs(out[~hit] - want[~hit]).max(initial=0) <= 8 * u       # (values of a few: the exact bounds are the other tests')
+
+
 def test_attention_far_pages():
     """A cache of more than 2^32 bytes: keys whose offsets pass 32 bits."""
     D, page, Hkv = 128, 256, 8
