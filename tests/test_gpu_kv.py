@@ -306,3 +306,145 @@ def test_other_stream():
         out = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, lse=lse, ws=ws)
     st.synchronize()
     check_attention(B, out, lse, what="another stream")
+
+
+def test_attention_many_sequences_chunks_among_them():
+    """More sequences than lanes, with a workspace: both kernels in one launch, single tokens and chunks in any order, empty slots between them."""
+    r = np.random.RandomState(1)
+    seqs = [(int(r.choice([0, 1, 1, 1, 2, 9, 40])), int(r.randint(0, 300))) for _ in range(140)]
+    seqs = [(n, n + c) for n, c in seqs]
+    for window, Hq, Hkv in ((0, 8, 2), (50, 4, 4)):
+        B = Batch(seqs, Hq, Hkv, 64, 16, window=window, seed=14, order="hnd").fill()
+        ws = serq.paged_attention_workspace(B.T, len(seqs), B.max_q, B.max_kv, Hq, Hkv, 64, DEV)
+        lse = torch.empty((B.T, Hq), device=DEV)
+        for use in (None, ws, ws):
+            out = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, window=window, lse=lse, ws=use)
+            check_attention(B, out, lse, what=f"many with chunks, window {window}")
+
+
+@pytest.mark.parametrize("name", ["ones", "few", "chunk", "long"])
+def test_attention_any_workspace(name):
+    """A workspace of any size serves, and the same one serves calls of any kind, one after the other."""
+    B = Batch(SETS[name], 8, 2, 128, 16, seed=15).fill()
+    C = Batch(SETS["chunk"], 4, 4, 64, 16, torch.float16, seed=16).fill()
+    full = serq.paged_attention_workspace(B.T, len(B.seqs), B.max_q, B.max_kv, 8, 2, 128, DEV).numel()
+    for n in (16, 32 << 10, (32 << 10) + 40000, (32 << 10) + 400000, full // 2, full, 2 * full + 1000000):
+        ws = torch.zeros(n, dtype=torch.uint8, device=DEV)
+        for X in (B, C, B):
+            lse = torch.empty((X.T, X.Hq), device=DEV)
+            out = serq.paged_attention(X.q, *X.args(), X.max_q, X.max_kv, lse=lse, ws=ws)
+            check_attention(X, out, lse, what=f"workspace of {n}")
+
+
+def test_attention_is_the_same_from_run_to_run():
+    """Slices are added in their order, whoever comes last."""
+    for seqs in ([(1, 9000)], [(100, 4000), (1, 700)], [(5, 3000), (2, 900)]):
+        B = Batch(seqs, 8, 2, 128, 16, seed=17).fill()
+        ws = serq.paged_attention_workspace(B.T, len(seqs), B.max_q, B.max_kv, 8, 2, 128, DEV)
+        want = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, ws=ws)
+        for _ in range(20):
+            assert torch.equal(serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, ws=ws), want)
+
+
+def test_lengths_past_the_table_are_cut():
+    B = Batch([(2, 64), (40, 64), (1, 30)], 4, 2, 64, 16, seed=18).fill()
+    B.seqs = [(2, 90), (40, 70), (1, 30)]                          # the table ends at 64
+    B.len = np.array([90, 70, 30], np.int32)
+    B.d_len.copy_(torch.from_numpy(B.len))
+    lse = torch.empty((B.T, 4), device=DEV)
+    out = serq.paged_attention(B.q, *B.args(), 40, 90, lse=lse)
+    check_attention(B, out, lse, what="cut")
+
+
+def test_nothing_to_do():
+    B = Batch([(0, 5), (0, 0)], 4, 2, 64, 16, seed=19)
+    assert serq.paged_attention(B.q, *B.args(), 0, 5).shape == (0, 4, 64)
+    assert serq.kv_append(B.q, B.k, B.v, *B.args()).shape == (0, 4, 64)
+    C = Batch([(3, 5)], 4, 2, 64, 16, seed=19)
+    none = torch.zeros((0, 1), dtype=torch.int32, device=DEV)
+    out = torch.full_like(C.q, 7.0)
+    serq.paged_attention(C.q, C.K, C.V, none, C.d_cu[:1], C.d_len[:0], 3, 5, out=out)
+    assert (out == 7).all()
+    # a cache without pages: no key can be seen
+    empty = torch.empty((0, 16, 2, 64), dtype=C.dt, device=DEV)
+    lse = torch.empty((3, 4), device=DEV)
+    assert not serq.paged_attention(C.q, empty, empty, C.d_table, C.d_cu, C.d_len, 3, 5, lse=lse).any() and torch.isneginf(lse).all()
+
+
+class _General:
+    def __getattr__(self, name):
+        return lambda *a: None
+
+
+def test_both_ways_from_python(monkeypatch):
+    """The extension module and ctypes: the same results, the same errors."""
+    B = Batch(RAGGED, 8, 2, 128, 16, fp8=True, seed=20).fill()
+    cos, sin = _tables(100, 128)
+    fast, got = serq._fast, []
+    for mod in (fast, _General()):
+        monkeypatch.setattr(serq, "_fast", mod)
+        K, V = B.K.clone(), B.V.clone()
+        q = serq.kv_append(B.q, B.k, B.v, K, V, *B.args()[2:], cos, sin, k_scale=B.k_scale, v_scale=B.v_scale)
+        ws = serq.paged_attention_workspace(B.T, len(B.seqs), B.max_q, B.max_kv, 8, 2, 128, DEV)
+        lse = torch.empty((B.T, 8), device=DEV)
+        out = serq.paged_attention(q, K, V, *B.args()[2:], B.max_q, B.max_kv, lse=lse, ws=ws, k_scale=B.k_scale, v_scale=B.v_scale)
+        got.append([q, K.view(torch.uint8), V.view(torch.uint8), out, lse])
+        for call, code in ((lambda: serq.paged_attention(B.q, *B.args(), 1, 1, scale=0.0), -3), (lambda: serq.paged_attention(B.q, *B.args(), 1, 1, window=-1), -3),
+                           (lambda: serq.paged_attention(B.q[:, :7], *B.args(), 1, 1), -3), (lambda: serq.kv_append(B.q, B.k, B.v, *B.args(), cos[:0], sin[:0]), -3),
+                           (lambda: serq.kv_append(B.q, B.k, B.v, *B.args(), cos[:, :4].contiguous(), sin[:, :4].contiguous()), -3)):
+            with pytest.raises(serq.SerqError) as e:
+                call()
+            assert e.value.code == code
+        t32 = B.d_table.long()
+        for call in (lambda: serq.paged_attention(B.q, B.K, B.V, t32, B.d_cu, B.d_len, 1, 1), lambda: serq.paged_attention(B.q, B.K, B.V[:1], *B.args()[2:], 1, 1),
+                     lambda: serq.paged_attention(B.q, *B.args()[:3], B.d_cu[:-1], B.d_len, 1, 1), lambda: serq.paged_attention(B.q.half(), B.K.float().bfloat16(), B.V.float().bfloat16(), *B.args()[2:], 1, 1),
+                     lambda: serq.paged_attention(B.q[..., :64], *B.args(), 1, 1), lambda: serq.paged_attention(B.q, *B.args(), 1, 1, out=B.q[:1]),
+                     lambda: serq.paged_attention(B.q, *B.args(), 1, 1, lse=torch.empty((B.T, 7), device=DEV)), lambda: serq.paged_attention(B.q, *B.args(), 1, 1, ws=torch.empty(64, device=DEV)),
+                     lambda: serq.paged_attention(B.q, *B.args(), 1, 1, k_scale=B.k_scale[:1]), lambda: serq.kv_append(B.q, B.k, B.v[:1], *B.args()),
+                     lambda: serq.kv_append(B.q, B.q, B.q, *B.args()), lambda: serq.kv_append(B.q, B.k, B.v, *B.args(), cos),
+                     lambda: serq.kv_append(B.q, B.k, B.v, *B.args(), cos.double(), sin.double()), lambda: serq.kv_append(B.q, B.k, B.v, *B.args(), cos, sin, positions=B.d_cu[:3])):
+            with pytest.raises(ValueError):
+                call()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_a_block_of_a_decoder(fp8):
+    """The example: prompts in one ragged call, then tokens through a replayed graph; against the same steps with plain attention on the cache."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "attention_block.py")
+    spec = importlib.util.spec_from_file_location("attention_block", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    block = ex.AttentionBlock(hidden=512, q_heads=8, kv_heads=2, dim=64, rank=32, pages=64, page=16, fp8=fp8)
+    prompts = [70, 3, 130]
+    seen = {}
+    real = serq.paged_attention
+
+    def spy(q, K, V, table, cu, kv_len, *a, **kw):
+        out = real(q, K, V, table, cu, kv_len, *a, **kw)
+        seen["last"] = (q, table, cu, kv_len, out)
+        if "first" not in seen:
+            seen["first"] = [t.clone() for t in seen["last"]]
+        return out
+
+    serq.paged_attention = spy
+    try:
+        first, y, kv_len, table, _ = ex.run(block, prompts, 5)
+    finally:
+        serq.paged_attention = real
+    assert kv_len.tolist() == [p + 1 + 5 for p in prompts] and torch.isfinite(first).all() and torch.isfinite(y).all()
+    for key, n in (("first", prompts), ("last", [1, 1, 1])):
+        q, tb, cu, ln, out = seen[key]
+        at = 0
+        for b in range(3):
+            L = int(ln[b])
+            p = torch.arange(L, device=DEV)
+            page, row = tb[b].long()[p // 16], p % 16
+            k, v = ((x.float() * (s[:, None] if s is not None else 1.0))[page, row].double().cpu().numpy() for x, s in ((block.K, block.k_scale), (block.V, block.v_scale)))
+            want, _, mag, big = orc.attention(q[at:at + n[b]].double().cpu().numpy(), k, v, 64 ** -0.5, L - n[b])
+            tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -7 + 2 * 72 * 2.0 ** -24 * big[..., None] + 2.0 ** -15) * mag
+            assert (np.abs(out[at:at + n[b]].double().cpu().numpy() - want) <= tol).all(), (key, b)
+            at += n[b]
