@@ -74,7 +74,10 @@ Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int
   const int64_t cus = device_cu_count();
   room = room > kTicketBytes ? room - kTicketBytes : 0;
   if (k.few) {
-    // as many workgroups as run together, each with an equal share of a head's keys; many more sequences than that are even enough by themselves
+    // As many workgroups as run together, each with an equal share of a head's keys; or a workgroup for every sequence and head, where sequences are
+    // many and short: a share then is several stretches, each of which has to get going, and the longest sequence is soon done with.  Measured (us, shares
+    // / whole sequences, 8 key heads, 512 run together, lengths up to 16 times apart): 70 up to 8000 140 / 232, 200 up to 4000 223 / 264, 250 up to
+    // 2000 141 / 151, 300 up to 1000 104 / 101, 600 up to 600 140 / 113, 1200 up to 600 309 / 238; 128 of 4000 356 / 359.
     const int64_t together = cus * paged_attn_few_resident(k.nb, f8, D), whole = (int64_t)seqs * heads;
     const int64_t slots = 2 * (int64_t)paged_attn_few_slot_floats(k.nb, D) * 4 * heads;   // bytes of a workgroup for each head
     const int64_t most = seqs * ((keys + kFewKeys - 1) / kFewKeys + 1);
@@ -83,7 +86,7 @@ Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int
     if (each > (int64_t)room / slots) each = (int64_t)room / slots;
     if (each > kTickets / heads) each = kTickets / heads;
     k.f = Plan{(int)whole, 1, 0, 0};
-    if (whole < 16 * together && each > 0) k.f = Plan{(int)each * heads, 2, kFewKeys, (size_t)(each * slots)};
+    if (whole * 256 < keys * together && each > 0) k.f = Plan{(int)each * heads, 2, kFewKeys, (size_t)(each * slots)};
     room -= k.f.bytes;
   }
   if (k.many) {

@@ -1,7 +1,8 @@
 // serq_paged_attn for batches that hold both chunks and single tokens: one launch in which some workgroups do the work of paged_attn_tile.h, bound by the
 // matrix instructions, and the others, beside them on the same compute units, that of paged_attn_few.h, bound by memory.  The first take
 // longest and start first.
-// Measured (us, one launch after the other / together): MEASURE
+// Measured (us, one launch after the other / together): a chunk of 384 after 3500 beside 7 single tokens, E4M3 cache, 67.6 / 53.8; 512 after up to 4000
+// beside 30 single tokens 108 / 86; 2000 after 4000 beside 6 170 / 157.
 #include "paged_attn_few.h"
 #include "paged_attn_tile.h"
 
