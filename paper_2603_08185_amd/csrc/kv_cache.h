@@ -68,21 +68,6 @@ inline int kv_check(const serq_kv_cache* c, const serq_kv_batch* b, int dtype, K
   return SERQ_OK;
 }
 
-// How many of the n sequences end at or before a place `at`, where sequence b ends at end(b), which does not decrease: the number of the
-// sequence that `at` lies in (n: none).  Uniform over the wave; one round of loads for 64 sequences.
-template <class End>
-__device__ __forceinline__ int sequences_before(int at, int n, int lane, const End& end) {
-  int b = 0;
-  while (b < n) {
-    const int i = b + lane;
-    const bool before = i < n && end(i) <= at;
-    const int c = __builtin_popcountll(__ballot(before));
-    b += c;
-    if (c < 64) break;
-  }
-  return b;
-}
-
 // two fp32 values as E4M3 bytes in the low (HI = false) or high half of `old`: clipped to +-448, ties to even, NaN stays NaN
 __device__ __forceinline__ float clip_e4m3(float x) { return x != x ? x : fminf(fmaxf(x, -448.0f), 448.0f); }
 template <bool HI>

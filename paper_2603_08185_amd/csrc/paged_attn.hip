@@ -8,7 +8,9 @@ namespace {
 constexpr int kTickets = 4096;
 constexpr size_t kTicketBytes = 2 * kTickets * 4;
 
-constexpr int kFewKeys = 256;                                 // keys of a share of the kernel for few rows, at least
+// Keys of a share of the kernel for few rows, at least: a share of its own costs its start and the meeting, a longer one more rounds of loads.
+// Measured with 128 / 256 / 512 / 1024 (us, one token, 8 key heads): 1000 keys 8.4 / 8.8 / 10.9 / 13.7, 8000 keys 16.1 / 13.4 / 16.1 / 23.2.
+constexpr int kFewKeys = 256;
 
 // (rows fit 31 bits, the threads of a grid 32)
 bool counts_ok(int64_t tokens, int64_t seqs, int q_heads, int heads) {
@@ -64,6 +66,9 @@ Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int
   if (max_q > tokens) max_q = (int)tokens;
   if (max_kv > 0x7fffffff) max_kv = 0x7fffffff;
   const int64_t rows = (int64_t)max_q * group;
+  // The kernel for few rows holds 16 or 32 of them.  Measured on sequences of 17 to 32 (us, few rows / many; 4 rows a token): 1 of 8 tokens after 4000
+  // 25.1 / 27.9, 1 of 6 after 30000 56.3 / 68.1, 1 of 5 after 300 13.1 / 10.2, 4 of 5 after 3000 29.3 / 26.1: it holds its own where keys are many, and
+  // one launch then serves drafts beside single tokens.
   k.many = rows > 32;
   k.few = !k.many || (seqs > 1 && tokens < (int64_t)max_q * seqs);   // (a sequence alone, or all alike: none is short)
   // beside a chunk, what is short is a token or a few

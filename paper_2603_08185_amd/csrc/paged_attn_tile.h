@@ -3,13 +3,22 @@
 // A workgroup takes 128 rows of a key head -- its four waves 32 each -- and a slice of the keys, in tiles of 64.  K and V of a tile lie in LDS, two
 // tiles deep: while one is used, the next is on its way (straight to LDS for 16-bit caches; through registers, where they become 16-bit
 // values, for E4M3 ones).  The scores of the next tile are computed while the present one's become weights: a matrix instruction, a pair of
-// weights, the load of an operand four instructions further on, and so forth (in that order by hand: the compiler's put each operand's load
+// weights, the load of an operand some instructions further on, and so forth (in that order by hand: the compiler's put each operand's load
 // right before its use).
 //   scores   S^T = K Q^T on the 32x32x16 instruction: a lane's results are 16 of 32 keys of one row, the other 16 are with the lane 32 further.
 //   weights  as in the kernel for few rows: exp2(s c - m c), m raised only when a score exceeds it by more than 2^6 in weight.
 //   values   O^T = V^T P^T: the weights are the instruction's operand as they stand (eight registers of scores become one operand of 16 keys in
 //            the order 4h .. 4h+3, 8+4h .. 8+4h+3), and V is read by columns in the same order.
 // The 16-byte pieces of a row in LDS are turned by the row's number, so that the lanes that read together meet different banks.
+//
+// 32 query and 8 key heads of 128 channels: a prompt of 8192 tokens 482 us (1.14 PFLOP/s; a large bf16 matrix product reaches 1.4 to 1.6), 512 tokens after
+// 32000 247 us (1.09), 4096 131 us (1.05); E4M3 cache 529, 64 channels 295 (0.93: as many exponentials for half the products).  The clock falls
+// as the matrix units get busier (2.1 to 1.9 GHz): the bound is power.  What carried it (us, before / after, prompt of 8192 unless stated): loads four
+// products ahead and the next scores beside the weights 538 / 518, the largest score beside the products with V 528 / 524, the wave
+// at its weights before the one at its products 524 / 506 (512 after 32000: 278 / 258).  Two waves share a SIMD, of two workgroups, so that
+// one is at the exponentials while the other multiplies.
+// Tried and not kept: eight waves on a tile, which halves the loads (511 against 508, E4M3 564 against 536), 64 rows a wave (530 registers spilled), some
+// of the weights beside the products with V (493 against 492), six operands ahead (487 against 484).  Without any loads it takes 451 of 518.
 #pragma once
 
 #include <type_traits>
