@@ -1,4 +1,6 @@
 // serq_paged_attn: argument checks, the choice of kernel and of the slices of a long cache (include/serq_kv.h; the kernels say what they do).
+#include <math.h>
+
 #include "paged_attn.h"
 
 namespace serq {
@@ -10,7 +12,15 @@ constexpr size_t kTicketBytes = 2 * kTickets * 4;
 
 // Keys of a share of the kernel for few rows, at least: a share of its own costs its start and the meeting, a longer one more rounds of loads.
 // Measured with 128 / 256 / 512 / 1024 (us, one token, 8 key heads): 1000 keys 8.4 / 8.8 / 10.9 / 13.7, 8000 keys 16.1 / 13.4 / 16.1 / 23.2.
+// Whoever joins a sequence reads a slot of all its rows for each of its shares, so the time that grows with the keys of a share stands against one that grows
+// with rows and shares: the least of both lies where the square of a share's keys is as rows times keys.  Measured (us, 256 / such shares / their keys
+// squared twice that): 8 tokens of 4 rows over 32000 keys, 8 key heads, 66.9 / 50.1 / 53.7; one token over 60000, one key head of 32 rows 124.7 / 53.4 / 54.9,
+// of 8 rows 40.5 / 27.6 / 28.0; over 30000, two key heads of 16 rows, 41.6 / 29.8 / 30.6.
 constexpr int kFewKeys = 256;
+int64_t few_keys(int64_t rows, int64_t keys) {
+  const int64_t n = (int64_t)sqrt((double)rows * (double)keys);
+  return n > kFewKeys ? (n + 63) / 64 * 64 : kFewKeys;
+}
 
 // (rows fit 31 bits, the threads of a grid 32)
 bool counts_ok(int64_t tokens, int64_t seqs, int q_heads, int heads) {
@@ -87,11 +97,16 @@ Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int
     const int64_t slots = 2 * (int64_t)paged_attn_few_slot_floats(k.nb, D) * 4 * heads;   // bytes of a workgroup for each head
     const int64_t most = seqs * ((keys + kFewKeys - 1) / kFewKeys + 1);
     int64_t each = (together + heads - 1) / heads;
+    // Where a sequence's parts and rows are many, a workgroup for every compute unit: half as many slots meet, and a unit streams as fast alone.  Measured (us,
+    // as many as run together / one a unit, 8 key heads): 1 token over 131000 88.3 / 84.3, over 32000 32.8 / 29.9, 8 over 130000 134.9 / 115.9, 4 of 8
+    // tokens over 8000 53.5 / 44.4; one token each of 255 sequences of up to 2000 157 / 163.
+    const int64_t rows_few = rows <= k.few_rows ? rows : group;
+    if (seqs > 0 && each / seqs * rows_few >= 256) each = (cus + heads - 1) / heads;
     if (each > most) each = most;
     if (each > (int64_t)room / slots) each = (int64_t)room / slots;
     if (each > kTickets / heads) each = kTickets / heads;
     k.f = Plan{(int)whole, 1, 0, 0};
-    if (whole * 256 < keys * together && each > 0) k.f = Plan{(int)each * heads, 2, kFewKeys, (size_t)(each * slots)};
+    if (whole * 256 < keys * together && each > 0) k.f = Plan{(int)each * heads, 2, (int)few_keys(rows_few, keys), (size_t)(each * slots)};
     room -= k.f.bytes;
   }
   if (k.many) {

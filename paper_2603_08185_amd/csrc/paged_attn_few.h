@@ -14,14 +14,15 @@
 //            through LDS, which reads it back by columns.
 // Weights are rounded to the 16-bit type for the product (that is what the instruction takes; the sums are fp32); their sum takes them unrounded.
 //
-// Bound by memory: 32 query and 8 key heads of 128 channels, one token a sequence: one of 131000 keys 88 us (6.1 TB/s; a plain read of as much reaches
+// Bound by memory: 32 query and 8 key heads of 128 channels, one token a sequence: one of 131000 keys 84 us (6.4 TB/s; a plain read of as much reaches
 // 6.7), 47 of up to 8000 106 us (5.2), 31 of up to 16000 with an E4M3 cache 77 us (5.4), 128 of 4000 356 us (5.9).  One token over 1000 keys: 9 us, of which
 // a chain of loads (lengths, pages, keys, the other shares' sums) is most.  By [page, head, row] the same batch is read 10 % faster than by
 // [page, row, head].  What carried it (us, without / with): equal shares against slices of the longest sequence's length 149 / 117 (47 sequences), loads
 // that do not stay in the caches 103.5 / 92 (one of 131000), the next tile's loads sent without a condition and shares that keep to a key head
-// 92 / 88.  Workgroups a compute unit: 1 / 2 / 4 84.5 / 88 / 93 (one of 131000), 163 / 157 / 167 (255 of up to 2000).
+// 92 / 88, and one workgroup a compute unit where the parts of a sequence are many 88 / 84.  (Workgroups a compute unit: 1 / 2 / 4 84.5 / 88 / 93 for one of
+// 131000, 163 / 157 / 167 for 255 of up to 2000.)  8 tokens over 32000: 50 us; with twice the shares 67, of which the join of 64 slots of 32 rows is half.
 // Tried and not kept: the next stretch's first loads before the present one's end (18.6 against 15.6 over 8000 keys: registers), shares that begin
-// with sequences (77 / 90 for the 31), three workgroups a compute unit by fewer registers (122 against 103 over 131000).
+// with sequences (77 / 90 for the 31), a join in two steps (8 tokens over 32000 46 with twice the shares, but 9.0 -> 9.5 over 1000 keys: code and registers), three workgroups a compute unit by fewer registers (122 against 103 over 131000).
 #pragma once
 
 #include <type_traits>
