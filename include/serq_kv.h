@@ -13,7 +13,8 @@
  * token i of sequence b is at position p = L_b - n_b + i.  Position p of sequence b lives in page table[b, p / page_size],
  * row p % page_size.  cu_q, kv_len and table lie in device memory, so that a captured graph can be replayed for the
  * next step; they are not checked on the host.  A sequence without new tokens is an empty slot.  cu_q must not decrease.
- * Rows of q from cu_q[seqs] on belong to no sequence: nothing is written for them.
+ * Rows of q, k and v before cu_q[0] and from cu_q[seqs] on belong to no sequence: nothing is written for them.  So a later part of
+ * cu_q, kv_len and table serves some of a batch's sequences over the buffers of all.
  */
 #ifndef SERQ_KV_H_
 #define SERQ_KV_H_

@@ -76,6 +76,7 @@ __global__ __launch_bounds__(512) void kv_append_kernel(AppendParams p) {
     len = p.c.len[i];
   };
   int b = 0, pos, end, len;
+  const int first = p.c.cu[0];                                // rows before it are of no sequence
   ask(0, end, len);
   int it = threadIdx.x;
   Item m{};
@@ -83,6 +84,7 @@ __global__ __launch_bounds__(512) void kv_append_kernel(AppendParams p) {
   __builtin_amdgcn_sched_barrier(0);
 
   // the token's sequence: the first that ends behind it
+  if (t < first) return;
   for (;;) {
     const int c = __builtin_popcountll(__ballot(b + lane < p.c.seqs && end <= t));
     b += c;

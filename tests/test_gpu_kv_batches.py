@@ -1,0 +1,52 @@
+"""Batches for the paged cache that a server hands over besides whole ones: a later part of a batch over the whole batch's buffers."""
+import pytest
+import torch
+
+from paper_2603_08185_amd import binding as serq
+from tests._kv import DEV, Batch, check_attention
+from tests.test_gpu_kv import _bits, _expected_append, _tables
+
+pytestmark = pytest.mark.gpu
+
+# the first sequence that is left has more keys than there are rows before it, so that a row taken for one of its own would find a place
+PART = [(3, 5), (2, 33), (1, 40), (0, 9), (17, 60), (1, 100)]
+CHUNKS = [(3, 5), (40, 90), (1, 70), (33, 150), (0, 0), (2, 300)]
+
+
+def _later(B, n):
+    """The sequences from n on; the rows of those before them belong to no sequence now."""
+    B.cu, B.len, B.table, B.seqs = B.cu[n:], B.len[n:], B.table[n:], B.seqs[n:]
+    B.d_cu, B.d_len, B.d_table = B.d_cu[n:], B.d_len[n:], B.d_table[n:]
+    return B
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("first", [1, 2, 4, 6])
+def test_append_a_later_part_of_a_batch(first, fp8):
+    B = _later(Batch(PART, 8, 2, 128, 16, fp8=fp8, extra=2, seed=21), first)
+    cos, sin = _tables(100, 128)
+    want_q, want_K, want_V, seq = _expected_append(B, cos, sin, False)
+    q_out = torch.full((B.T, 8, 128), 7.0, dtype=B.dt, device=DEV)
+    serq.kv_append(B.q, B.k, B.v, *B.args(), cos, sin, k_scale=B.k_scale, v_scale=B.v_scale, q_out=q_out)
+    mine = torch.from_numpy(seq >= 0)
+    assert int(mine.sum()) == B.cu[-1] - B.cu[0] and (q_out[~mine.to(DEV)] == 7).all()
+    assert torch.equal(_bits(q_out.cpu()[mine]), _bits(want_q[mine]))
+    for got, want in ((B.K, want_K), (B.V, want_V)):              # (places that nothing was appended to hold NaN)
+        got, nan = got.cpu().contiguous(), torch.isnan(want.float())
+        assert torch.equal(nan, torch.isnan(got.float())) and torch.equal(_bits(got)[~nan], _bits(want)[~nan])
+
+
+@pytest.mark.parametrize("seqs", [PART, CHUNKS])
+@pytest.mark.parametrize("first", [1, 2, 3])
+def test_attention_a_later_part_of_a_batch(seqs, first):
+    B = Batch(seqs, 8, 2, 128, 16, extra=1, seed=22).fill()
+    B.kv, B = B.kv[first:], _later(B, first)
+    ws = serq.paged_attention_workspace(B.T, len(B.seqs), B.max_q, B.max_kv, 8, 2, 128, DEV)
+    for use in (None, ws):
+        out, lse = torch.full((B.T, 8, 128), 7.0, dtype=B.dt, device=DEV), torch.full((B.T, 8), 7.0, device=DEV)
+        serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, out=out, lse=lse, ws=use)
+        none = torch.ones(B.T, dtype=torch.bool, device=DEV)
+        none[B.cu[0]:B.cu[-1]] = False
+        assert (out[none] == 7).all() and (lse[none] == 7).all()
+        out[none], lse[none] = 0, -float("inf")                   # (as the oracle has a row of no sequence)
+        check_attention(B, out, lse, what=f"from sequence {first} on")
