@@ -479,7 +479,8 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, int count, cha
     const RowBlock k = row_block<BM>(p, x.b, x.c0, x.n, x.L, 0);
     const int ends = x.before + x.pieces, until = min(stop, ends), base = k.begin & ~15;
     const bool cut = at > x.before || until < ends;
-    const int k0 = base + (at - x.before) * kUnit, k1 = until < ends ? base + (until - x.before) * kUnit : max(k.end, 0);
+    // (a sequence of more tokens than max_q has pieces past what the block's rows see, maybe nothing that they see: no table entry is read there)
+    const int end = max(k.end, 0), k0 = base + (at - x.before) * kUnit, k1 = until < ends ? min(base + (until - x.before) * kUnit, end) : end;
     Part<BM * (D + 2)> part{};
     if (cut) {
       const int first = x.before / share;

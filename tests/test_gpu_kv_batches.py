@@ -50,3 +50,23 @@ def test_attention_a_later_part_of_a_batch(seqs, first):
         assert (out[none] == 7).all() and (lse[none] == 7).all()
         out[none], lse[none] = 0, -float("inf")                   # (as the oracle has a row of no sequence)
         check_attention(B, out, lse, what=f"from sequence {first} on")
+
+
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("n,L", [(1000, 500), (700, 5000), (300, 0), (90, 89)])
+def test_more_tokens_than_max_q_stay_in_bounds(n, L, window):
+    """Wrong results are all that such a call may give: a sequence whose first tokens lie before its start (a length that has been cut) has no key that its
+    first block of rows sees, though its length counts many.  Nothing beside the batch's rows is written, and the workspace is ready for the next call."""
+    good = Batch([(1, 700), (2, 900)], 8, 2, 128, 16, window=window, seed=23).fill()
+    B = Batch([(1, 300), (n, max(L, n)), (2, 90)], 8, 2, 128, 16, window=window, seed=24, extra=3)
+    B.d_len[1] = L
+    table = torch.zeros((B.d_table.shape[0], B.width + 8), dtype=torch.int32, device=DEV)[:, :B.width]
+    ws = serq.paged_attention_workspace(B.T, len(B.seqs), 2, max(L, 900), 8, 2, 128, DEV)
+    for use in (None, ws):
+        big = torch.full((B.T, 9, 136), 7.0, dtype=B.dt, device=DEV)
+        lse = torch.full((B.T, 8), 7.0, device=DEV)
+        serq.paged_attention(B.q, B.K, B.V, table, B.d_cu, B.d_len, 2, max(L, 900), window=window, out=big[:, :8, :128], lse=lse, ws=use)
+        assert (big[:, 8:] == 7).all() and (big[:, :, 128:] == 7).all() and (big[-3:] == 7).all() and (lse[-3:] == 7).all()
+    lse = torch.empty((good.T, 8), device=DEV)
+    out = serq.paged_attention(good.q, *good.args(), good.max_q, good.max_kv, window=window, lse=lse, ws=ws)
+    check_attention(good, out, lse, what="the call after it")
