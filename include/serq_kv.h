@@ -48,7 +48,7 @@ typedef struct serq_kv_batch {
   const int32_t* table;           /* [seqs, table_width], row stride table_ld */
   int64_t        table_ld;
   int64_t        tokens;          /* rows of q, k, v and out: 0 .. 2^22 */
-  int32_t        table_width;
+  int32_t        table_width;     /* table_width * page_size up to 2^31 - 2^23 */
   int32_t        seqs;            /* 0 .. 65536 */
 } serq_kv_batch;
 

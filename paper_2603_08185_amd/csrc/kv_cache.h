@@ -19,6 +19,9 @@ struct KvView {
 
 constexpr int64_t kKvTokens = 1 << 22;   // of a call (a workgroup of up to 512 threads each: a grid's threads are counted in 32 bits)
 
+// of a table: positions are 32-bit numbers, and the kernels look up to 64 tiles past a sequence's end before they cut a position to it
+constexpr int64_t kKvPositions = (1ll << 31) - (1 << 23);
+
 inline bool kv_aligned(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 // q, k, v, out: a token's and a head's stride in elements
@@ -38,7 +41,7 @@ inline int kv_check(const serq_kv_cache* c, const serq_kv_batch* b, int dtype, K
   if (c->heads < 1 || c->heads > 1024 || c->pages < 0 || c->pages > 0x7fffffff) return SERQ_ESHAPE;
   if (c->page_size < 16 || c->page_size > 65536 || (c->page_size & (c->page_size - 1))) return SERQ_ESHAPE;
   if (b->seqs < 0 || b->seqs > 65536 || b->tokens < 0 || b->tokens > kKvTokens || b->table_width < 0) return SERQ_ESHAPE;
-  if ((int64_t)b->table_width * c->page_size > 0x7fffffff || b->table_ld < b->table_width) return SERQ_ESHAPE;
+  if ((int64_t)b->table_width * c->page_size > kKvPositions || b->table_ld < b->table_width) return SERQ_ESHAPE;
   const int64_t unit = c->dtype == SERQ_F8 ? 16 : 8, es = c->dtype == SERQ_F8 ? 1 : 2;
   const int64_t st[6] = {c->k_page, c->k_token, c->k_head, c->v_page, c->v_token, c->v_head};
   for (int64_t s : st) {
