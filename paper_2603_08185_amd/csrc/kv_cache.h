@@ -19,7 +19,8 @@ struct KvView {
 
 constexpr int64_t kKvTokens = 1 << 22;   // of a call (a workgroup of up to 512 threads each: a grid's threads are counted in 32 bits)
 
-// of a table: positions are 32-bit numbers, and the kernels look up to 64 tiles past a sequence's end before they cut a position to it
+// of a table: positions are 32-bit numbers, and the kernels look up to 64 tiles past a sequence's end before they cut a position to it, and
+// a window short of it and kKvTokens before its start
 constexpr int64_t kKvPositions = (1ll << 31) - (1 << 23);
 
 inline bool kv_aligned(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }

@@ -152,6 +152,8 @@ int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int d
   p.ldq = 2 * ldq; p.ldqh = 2 * ldqh; p.ldo = 2 * ldo; p.ldoh = 2 * ldoh;
   p.q_heads = q_heads; p.group = q_heads / cache->heads; p.window = window; p.scale = scale;
   const bool f8 = cache->dtype == SERQ_F8;
+  // (as wide as the table or wider: it hides nothing, and the position of a token before the start less such a window would not fit 32 bits)
+  if (window >= (int64_t)batch->table_width * cache->page_size) p.window = window = 0;
   if (!workspace) workspace_bytes = 0;
   const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, window, cache->heads, p.group, D, f8, workspace_bytes);
   AttnParams few = p, many = p;

@@ -70,3 +70,15 @@ def test_more_tokens_than_max_q_stay_in_bounds(n, L, window):
     lse = torch.empty((good.T, 8), device=DEV)
     out = serq.paged_attention(good.q, *good.args(), good.max_q, good.max_kv, window=window, lse=lse, ws=ws)
     check_attention(good, out, lse, what="the call after it")
+
+
+@pytest.mark.parametrize("seqs", [[(3, 2), (8, 3), (1, 50), (5, 5)], [(60, 20), (1, 50), (40, 40)]])
+@pytest.mark.parametrize("window", [(1 << 31) - 1, (1 << 31) - 3, 1 << 30, 101])
+def test_a_window_that_reaches_past_the_start_is_none(seqs, window):
+    """Also where the first new tokens lie before the start of their sequence."""
+    B = Batch(seqs, 8, 2, 128, 16, seed=25, extra=0).fill()
+    ws = serq.paged_attention_workspace(B.T, len(B.seqs), B.max_q, B.max_kv, 8, 2, 128, DEV)
+    for use in (None, ws):
+        lse = torch.full((B.T, 8), 7.0, device=DEV)
+        out = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, window=window, lse=lse, ws=use)
+        check_attention(B, out, lse, what=f"window {window}")
