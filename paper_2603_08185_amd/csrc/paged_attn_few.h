@@ -9,7 +9,7 @@
 //   scores   S^T = K Q^T on the 16x16x32 matrix instruction: keys are its rows, fetched from memory in the layout of its operand (a lane has
 //            16 bytes of one key), queries its columns, so that a lane's results are 4 keys of one row.
 //   weights  exp2(s c - m c), c = scale log2 e: one fused multiply-add and one exponential.  m is raised only when a score exceeds it by more than
-//            2^6 in weight; between two raises no lane needs another's maximum.
+//            2^6 in weight; between two raises no lane needs another's maximum.  (fp16: 2^9 times that, so that small ones keep their bits.)
 //   values   O^T = V^T P^T: the lane's weights are the instruction's operand as they stand (8 keys: 4 of one group of 16, 4 of the next); V goes
 //            through LDS, which reads it back by columns.
 // Weights are rounded to the 16-bit type for the product (that is what the instruction takes; the sums are fp32); their sum takes them unrounded.
@@ -248,7 +248,7 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
   };
 
   v4f o[NB][D / 16];
-  float m[NB], sum[NB];                                       // the reference times c; the lane's part of the sum of weights
+  float m[NB], sum[NB];                                       // the reference in the exponent; the lane's part of the sum of weights
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     m[nb] = -FLT_MAX;
@@ -351,7 +351,7 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
       if (__ballot(top > ref[nb] + slack)) {
         const float now = fmaxf(ref[nb], quads_reduce(top, [](float x, float y) { return fmaxf(x, y); }));
         ref[nb] = now;
-        const float mc = fmaxf(now * c, -FLT_MAX), f = exp2_fast(m[nb] - mc);
+        const float mc = reference<DT>(now, c), f = exp2_fast(m[nb] - mc);
         m[nb] = mc;
         sum[nb] *= f;
 #pragma unroll

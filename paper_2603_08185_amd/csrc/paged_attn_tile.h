@@ -188,7 +188,7 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
   for (int d = 0; d < DB; ++d)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
-  float ref = -FLT_MAX, m = -FLT_MAX;                         // the reference as a score, times c
+  float ref = -FLT_MAX, m = -FLT_MAX;                         // the reference as a score, in the exponent
   float sum = 0.0f, sum2 = 0.0f;                              // the lane's part of the sum of weights: even and odd ones
 
   const int krow = n32 * ROW, kturn = (half ^ turn_k<D>(n32)) << 4;
@@ -258,7 +258,7 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
       const uint32_t bits = __float_as_uint(top);
       const auto two = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
       ref = fmaxf(ref, fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])));
-      const float mc = fmaxf(ref * c, -FLT_MAX), f = exp2_fast(m - mc);
+      const float mc = reference<DT>(ref, c), f = exp2_fast(m - mc);
       m = mc;
       sum *= f;
       sum2 *= f;

@@ -1,4 +1,5 @@
 """Batches for the paged cache that a server hands over besides whole ones: a later part of a batch over the whole batch's buffers."""
+import numpy as np
 import pytest
 import torch
 
@@ -82,3 +83,39 @@ def test_a_window_that_reaches_past_the_start_is_none(seqs, window):
         lse = torch.full((B.T, 8), 7.0, device=DEV)
         out = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, window=window, lse=lse, ws=use)
         check_attention(B, out, lse, what=f"window {window}")
+
+
+def _sink(n, L, Hq, Hkv, D, gap, page=64, seed=0):
+    """A key that dominates, and L - 1 others that each weigh 2^-gap of it and together a good part of the sum: q is one channel of ones, the first key is 0
+    there and the others -gap ln 2 / scale.  Values: 0 for the first key, 1 + |noise| / 4 for the others, so that what their weights lose shows."""
+    B = Batch([(n, L)], Hq, Hkv, D, page, torch.float16, seed=seed).fill()
+    B.qkv[:, :Hq * D] = 0
+    B.q[..., 0] = 1
+    k = torch.zeros(L, Hkv, D)
+    k[1:, :, 0] = -gap * float(np.log(2.0)) * D ** 0.5
+    v = 1 + torch.randn(L, Hkv, D, generator=torch.Generator().manual_seed(seed)).abs() / 4
+    v[0] = 0
+    at = np.arange(L)
+    where, row = torch.from_numpy(B.table[0, at // page]).to(DEV), torch.from_numpy(at % page).to(DEV)
+    for cache, x in ((B.K, k), (B.V, v)):
+        cache[where, row] = x.half().to(DEV)
+    B.kv = [[x.half().double().numpy() for x in (k, v)]]
+    return B
+
+
+# gap: weights of 2^-gap of the largest; 2^-20.5 is 11.3 steps of an fp16 number below 2^-14, 2^-24.4 three quarters of one
+@pytest.mark.parametrize("gap", [17.97, 20.5, 24.4])
+@pytest.mark.parametrize("n,Hq,Hkv,sliced", [(1, 4, 1, True), (1, 4, 1, False), (40, 2, 1, False), (40, 2, 1, True)])
+def test_small_weights_beside_a_large_one_in_fp16(n, Hq, Hkv, sliced, gap):
+    """Weights meet V as 16-bit numbers: bits of them may go, not parts of the result.  Errors, derived: the result's rounding, 2^-11 |out|; a weight's, 2^-11 of it or,
+    below 2^-23 of the largest, half a step there, 2^-34 of the largest; the score, one product that is exact but for 2^-23 of its 17 to 25 in the exponent, twice: 2^-17
+    of a weight; exponential, running factors and sums (32 + L / 16) 2^-22."""
+    L, D = 60000, 128
+    B = _sink(n, L, Hq, Hkv, D, gap)
+    ws = serq.paged_attention_workspace(B.T, 1, n, L, Hq, Hkv, D, DEV) if sliced else None
+    lse = torch.empty((n, Hq), device=DEV)
+    out = serq.paged_attention(B.q, *B.args(), n, L, lse=lse, ws=ws).double().cpu().numpy()
+    want, wlse, mag, _ = B.attention64()
+    rel = 2.0 ** -11 + 2.0 ** (gap - 34) + 2.0 ** -17 + (32 + L / 16) * 2.0 ** -22
+    assert (np.abs(out - want) <= 2.0 ** -11 * np.abs(want) + rel * mag).all(), np.abs(out / want - 1).max()
+    assert (np.abs(lse.double().cpu().numpy() - wlse) <= 2.0 ** -17 + (32 + L / 16) * 2.0 ** -22 + 2.0 ** -20).all()
