@@ -128,11 +128,15 @@ __device__ __forceinline__ float quads_reduce(float v, const Op& op) {
   return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+constexpr float kLog2e = 1.44269504088896341f;
+
 // Weights are 16-bit numbers where they meet V.  bf16 has exponents for all of them; fp16 ends at 2^16 and loses bits below 2^-14, so there the reference lies
 // 9 lower in the exponent: weights are at most 2^15, and of full precision down to 2^-23 of the reference's own.  (Else 60000 keys
 // 20.5 below in the exponent, 2^-20.5 being 11.3 of the type's smallest steps, would each count as 11.)
 template <int DT> constexpr float kHeadroom = DT == SERQ_F16 ? 9.0f : 0.0f;
 template <int DT> __device__ __forceinline__ float reference(float score, float c) { return fmaxf(score * c - kHeadroom<DT>, -FLT_MAX); }
+// what makes a score one in the exponent of 2 (not 0, which would make NaN of a masked score)
+__device__ __forceinline__ float score_factor(float scale, float k_scale) { return fmaxf(scale * k_scale * kLog2e, FLT_MIN); }
 // by how much a score may exceed the reference before that is raised: 2^6 in weight
 __device__ __forceinline__ float score_slack(float c) { return fminf(6.0f / c, 1e30f); }
 
@@ -197,7 +201,6 @@ __device__ __forceinline__ float row_lse(float m, float l) {
 constexpr int kMaxSlices = 256;          // of the kernel for few rows
 constexpr int kMaxTileSlices = 32;       // of the kernel for many
 constexpr int kTileRows = 128;
-constexpr float kLog2e = 1.44269504088896341f;
 
 // ---- where the slices of a row block meet -------------------------------------------------------------------------------------
 // A slice leaves its weighted sums and the statistics (m, l) of its rows in a slot of the workspace: rows x D floats in an order of the kernel's own,

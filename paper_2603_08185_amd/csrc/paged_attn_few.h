@@ -201,7 +201,7 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
   }
   const int all_lo = k.all_from, all_hi = k.all_to;           // no mask there
   const float ks = p.c.k_scale ? p.c.k_scale[h] : 1.0f, vs = p.c.v_scale ? p.c.v_scale[h] : 1.0f;
-  const float c = p.scale * ks * kLog2e, slack = score_slack(c);
+  const float c = score_factor(p.scale, ks), slack = score_slack(c);
 
   const char* kbase = p.c.k + h * p.c.k_head;
   const char* vbase = p.c.v + h * p.c.v_head;

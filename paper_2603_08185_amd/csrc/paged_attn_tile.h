@@ -104,7 +104,7 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
   const int wr0 = k.r0 + 32 * w, wr1 = min(k.r0 + k.rows, wr0 + 32) - 1;
   const int all_lo = p.window > 0 ? max(0, first + wr1 / G - p.window + 1) : 0, all_hi = min(first + wr0 / G + 1, k.end);
   const float ks = p.c.k_scale ? p.c.k_scale[h] : 1.0f, vs = p.c.v_scale ? p.c.v_scale[h] : 1.0f;
-  const float c = p.scale * ks * kLog2e, slack = score_slack(c);
+  const float c = score_factor(p.scale, ks), slack = score_slack(c);
 
   // ---- loads: a wave brings LOADS * RPI rows of K and of V, which lie in one page
   const int mask = (1 << p.c.page_shift) - 1;

@@ -119,3 +119,13 @@ def test_small_weights_beside_a_large_one_in_fp16(n, Hq, Hkv, sliced, gap):
     rel = 2.0 ** -11 + 2.0 ** (gap - 34) + 2.0 ** -17 + (32 + L / 16) * 2.0 ** -22
     assert (np.abs(out - want) <= 2.0 ** -11 * np.abs(want) + rel * mag).all(), np.abs(out / want - 1).max()
     assert (np.abs(lse.double().cpu().numpy() - wlse) <= 2.0 ** -17 + (32 + L / 16) * 2.0 ** -22 + 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("seqs", [[(3, 5), (1, 40), (8, 130)], [(40, 90), (1, 70)]])
+@pytest.mark.parametrize("scale", [1.5e-45, 1e-40, 1e-37])
+def test_attention_the_smallest_scales(seqs, scale):
+    """Products of the scale with the cache's own that 32 bits do not hold: every key a row sees weighs the same."""
+    B = Batch(seqs, 8, 2, 128, 16, fp8=True, seed=26).fill()
+    lse = torch.empty((B.T, 8), device=DEV)
+    out = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, scale=scale, k_scale=B.k_scale, v_scale=B.v_scale, lse=lse)
+    check_attention(B, out, lse, scale, what=f"scale {scale}")
