@@ -89,9 +89,10 @@ int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_heads,
  *          depend on them but for the order of fp32 sums).  More tokens or keys than that give SERQ_OK and wrong results, but
  *          nothing is read or written out of bounds.
  *   lse    [tokens, q_heads] fp32, or NULL.
- *   workspace  serq_paged_attn_workspace_bytes(...) bytes prepared by serq_workspace_init: where the slices of long caches meet.
- *          NULL / 0, or too little, makes the call do without slices.  Left ready for the next call; two calls that share one must not
- *          overlap in time.
+ *   workspace  serq_paged_attn_workspace_bytes(...) bytes prepared by serq_workspace_init: where the slices of long caches meet.  What it
+ *          returns serves every call of up to as many tokens and sequences, max_q and max_kv, with the same heads: sized once for the largest step.
+ *          NULL / 0, or too little, makes the call do without slices, or with fewer.  Left ready for the next call; two calls that share one
+ *          must not overlap in time.
  */
 int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int dtype, const serq_kv_cache* cache,
                     const serq_kv_batch* batch, int max_q, int64_t max_kv, float scale, int window,

@@ -730,7 +730,7 @@ def kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, K: to
 
 
 def paged_attention_workspace(tokens: int, seqs: int, max_q: int, max_kv: int, q_heads: int, kv_heads: int, dim: int, device) -> torch.Tensor:
-    """A zeroed workspace for paged_attention (slices of a long cache)."""
+    """A zeroed workspace for paged_attention (slices of a long cache): for every call of up to these tokens, sequences and bounds."""
     n = lib().serq_paged_attn_workspace_bytes(tokens, seqs, max_q, max_kv, q_heads, kv_heads, dim)
     if n == 0:
         raise SerqError("serq_paged_attn_workspace_bytes", -3)

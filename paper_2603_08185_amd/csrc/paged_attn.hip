@@ -41,8 +41,8 @@ constexpr size_t kManyRoom = 46u << 20;                        // most that its 
 // sequence than may be needed (every sequence's last one is half empty on average); `full` is about what there is.
 // Measured (32 query and 8 key heads; us with 1 / 2 / 3 / 4 / 5 / 8 slices): 384 tokens after 3500 66.6 / 43.1 / 44.8 / 45.5 / 45.2 / 48.4, 100 after 30000
 // 469 / 245 / 171 / 134 / 114 / 87, 512 fresh ones 14.9 / 16.9 / 17.3 / 21.5; 512 after 32000 with 2 / 4 292 / 272, 256 after 8000 with 3 / 4 56.5 / 50.6.
+constexpr int64_t kGrain = 128;                                // keys of a slice are a multiple of it
 Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, size_t slot_floats, size_t room) {
-  constexpr int64_t kGrain = 128;
   Plan k{blocks, 1, 0x7fffff00, 0};
   const int64_t units = (int64_t)blocks * heads, slot = (int64_t)slot_floats * 4, bytes_most = (int64_t)(room < kManyRoom ? room : kManyRoom);
   if (units <= 0 || units > kTickets || keys <= kGrain) return k;
@@ -63,6 +63,16 @@ Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, s
   else k.slice_keys = 0x7fffff00;
   return k;
 }
+
+// Workgroups of the kernel for few rows for a key head, where `together` run together.
+int64_t few_shares(int64_t together, int seqs, int heads, int64_t keys) {
+  const int64_t most = seqs * ((keys + kFewKeys - 1) / kFewKeys + 1);
+  int64_t each = (together + heads - 1) / heads;
+  if (each > most) each = most;
+  return each > kTickets / heads ? kTickets / heads : each;
+}
+size_t few_slots_bytes(int64_t each, int heads, int nb, int D) { return (size_t)(each * heads) * 2 * paged_attn_few_slot_floats(nb, D) * 4; }
+int many_blocks(int64_t tokens, int seqs, int group) { return (int)(tokens * group / kTileRows) + seqs; }
 
 struct Plans {
   bool few, many;         // which kernels have work
@@ -94,28 +104,43 @@ Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int
     // / whole sequences, 8 key heads, 512 run together, lengths up to 16 times apart): 70 up to 8000 140 / 232, 200 up to 4000 223 / 264, 250 up to
     // 2000 141 / 151, 300 up to 1000 104 / 101, 600 up to 600 140 / 113, 1200 up to 600 309 / 238; 128 of 4000 356 / 359.
     const int64_t together = cus * paged_attn_few_resident(k.nb, f8, D), whole = (int64_t)seqs * heads;
-    const int64_t slots = 2 * (int64_t)paged_attn_few_slot_floats(k.nb, D) * 4 * heads;   // bytes of a workgroup for each head
-    const int64_t most = seqs * ((keys + kFewKeys - 1) / kFewKeys + 1);
-    int64_t each = (together + heads - 1) / heads;
+    const int64_t slots = (int64_t)few_slots_bytes(1, heads, k.nb, D);                    // bytes of a workgroup for each head
     // Where a sequence's parts and rows are many, a workgroup for every compute unit: half as many slots meet, and a unit streams as fast alone.  Measured (us,
     // as many as run together / one a unit, 8 key heads): 1 token over 131000 88.3 / 84.3, over 32000 32.8 / 29.9, 8 over 130000 134.9 / 115.9, 4 of 8
     // tokens over 8000 53.5 / 44.4; one token each of 255 sequences of up to 2000 157 / 163.
     const int64_t rows_few = rows <= k.few_rows ? rows : group;
-    if (seqs > 0 && each / seqs * rows_few >= 256) each = (cus + heads - 1) / heads;
-    if (each > most) each = most;
+    int64_t each = (together + heads - 1) / heads;
+    each = few_shares(seqs > 0 && each / seqs * rows_few >= 256 ? cus : together, seqs, heads, keys);
     if (each > (int64_t)room / slots) each = (int64_t)room / slots;
-    if (each > kTickets / heads) each = kTickets / heads;
     k.f = Plan{(int)whole, 1, 0, 0};
     if (whole * 256 < keys * together && each > 0) k.f = Plan{(int)each * heads, 2, (int)few_keys(rows_few, keys), (size_t)(each * slots)};
     room -= k.f.bytes;
   }
   if (k.many) {
-    const int blocks = (int)(tokens * group / kTileRows) + seqs;
+    const int blocks = many_blocks(tokens, seqs, group);
     // (sequences of about the longest one's length, and half of the last block of each)
     const int64_t alike = 2 * tokens / max_q < seqs ? 2 * tokens / max_q : seqs;
     k.m = plan_many(blocks, (tokens * group + kTileRows - 1) / kTileRows + (alike - 1) / 2, heads, keys, cus, paged_attn_tile_slot_floats(D), room);
   }
   return k;
+}
+
+// The most that a call of up to these sizes, with either cache and any window, takes of a workspace: a caller who sizes one for its largest step decodes with
+// the same one, so what matters is not this step's own plan (a long prompt alone needs no slices).
+size_t most_bytes(int64_t tokens, int seqs, int max_q, int64_t max_kv, int heads, int group, int D) {
+  const int64_t rows = (max_q < tokens ? max_q : tokens) * group, cus = device_cu_count();
+  if (max_kv > kKvPositions) max_kv = kKvPositions;
+  const int nb = rows > 16 ? 2 : 1;
+  const int resident = nb > 1 ? paged_attn_few_resident(nb, false, D) : paged_attn_few_resident(nb, true, D);   // (the larger one: E4M3)
+  size_t bytes = kTicketBytes + few_slots_bytes(few_shares(cus * resident, seqs, heads, max_kv), heads, nb, D);
+  if (rows > 32 && max_kv > kGrain) {
+    int64_t units = (int64_t)many_blocks(tokens, seqs, group) * heads, slices = (max_kv + kGrain - 1) / kGrain;
+    if (units > kTickets) units = kTickets;
+    if (slices > kMaxTileSlices) slices = kMaxTileSlices;
+    const size_t slots = (size_t)(units * slices) * paged_attn_tile_slot_floats(D) * 4;
+    bytes += slots < kManyRoom ? slots : kManyRoom;
+  }
+  return bytes;
 }
 
 }  // namespace
@@ -129,8 +154,7 @@ size_t serq_paged_attn_workspace_bytes(int64_t tokens, int seqs, int max_q, int6
   if (tokens < 0 || tokens > kKvTokens || seqs < 0 || seqs > 65536 || max_q < 0 || max_kv < 0 || kv_heads < 1 || kv_heads > 1024 ||
       q_heads < 1 || q_heads > 65535 || q_heads % kv_heads || (dim != 64 && dim != 128) || !counts_ok(tokens, seqs, q_heads, kv_heads))
     return 0;
-  const Plans k = plans(tokens, seqs, max_q, max_kv, 0, kv_heads, q_heads / kv_heads, dim, false, (size_t)1 << 40);
-  return kTicketBytes + k.f.bytes + k.m.bytes;
+  return most_bytes(tokens, seqs, max_q, max_kv, kv_heads, q_heads / kv_heads, dim);
 }
 
 int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int dtype, const serq_kv_cache* cache,

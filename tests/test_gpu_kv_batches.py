@@ -129,3 +129,16 @@ def test_attention_the_smallest_scales(seqs, scale):
     lse = torch.empty((B.T, 8), device=DEV)
     out = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, scale=scale, k_scale=B.k_scale, v_scale=B.v_scale, lse=lse)
     check_attention(B, out, lse, scale, what=f"scale {scale}")
+
+
+@pytest.mark.parametrize("seqs", [[(1, 9000)], [(5, 6000)], [(1, 4000), (1, 700), (1, 90)], [(100, 4000), (1, 700)], [(40, 3000)]])
+def test_the_workspace_of_the_largest_step_serves_the_others(seqs):
+    """Sized for a prompt of 8192 tokens, a long cache and a few users: smaller steps run as with all the room there could be."""
+    B = Batch(seqs, 8, 2, 128, 16, seed=27).fill()
+    ws = serq.paged_attention_workspace(8192, 4, 8192, 131072, 8, 2, 128, DEV)
+    room = torch.zeros(256 << 20, dtype=torch.uint8, device=DEV)
+    lse = torch.empty((B.T, 8), device=DEV)
+    want = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, ws=room)
+    out = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, lse=lse, ws=ws)
+    check_attention(B, out, lse, what="workspace of the largest step")
+    assert torch.equal(out, want)
