@@ -92,7 +92,8 @@ int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_heads,
  *   workspace  serq_paged_attn_workspace_bytes(...) bytes prepared by serq_workspace_init: where the slices of long caches meet.  What it
  *          returns serves every call of up to as many tokens and sequences, max_q and max_kv, with the same heads: sized once for the largest step.
  *          NULL / 0, or too little, makes the call do without slices, or with fewer.  Left ready for the next call; two calls that share one
- *          must not overlap in time.
+ *          must not overlap in time.  It is this function's own: what it keeps zero and what it leaves behind lie elsewhere than the layers' (serq_linear and
+ *          the like), so a buffer that goes from one to the other has to pass through serq_workspace_init in between.
  */
 int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int dtype, const serq_kv_cache* cache,
                     const serq_kv_batch* batch, int max_q, int64_t max_kv, float scale, int window,

@@ -175,6 +175,7 @@ def flags(path: int = PATH_AUTO, splitk: int = 0, groupm: int = 0, coltiles: int
 
 
 def workspace(M: int, N: int, K: int, r: int, abits: int, device) -> torch.Tensor:
+    """A zeroed workspace for linear (paged_attention has its own)."""
     n = lib().serq_workspace_bytes(M, N, K, r, abits)
     ws = torch.empty(max(n, 16), dtype=torch.uint8, device=device)
     _check("serq_workspace_init", lib().serq_workspace_init(_ptr(ws), ws.numel(), _stream()))
@@ -730,7 +731,8 @@ def kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, K: to
 
 
 def paged_attention_workspace(tokens: int, seqs: int, max_q: int, max_kv: int, q_heads: int, kv_heads: int, dim: int, device) -> torch.Tensor:
-    """A zeroed workspace for paged_attention (slices of a long cache): for every call of up to these tokens, sequences and bounds."""
+    """A zeroed workspace for paged_attention (slices of a long cache): for every call of up to these tokens, sequences and bounds.
+    Not for the layers: theirs is workspace()'s, and neither serves the other."""
     n = lib().serq_paged_attn_workspace_bytes(tokens, seqs, max_q, max_kv, q_heads, kv_heads, dim)
     if n == 0:
         raise SerqError("serq_paged_attn_workspace_bytes", -3)

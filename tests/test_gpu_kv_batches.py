@@ -142,3 +142,27 @@ def test_the_workspace_of_the_largest_step_serves_the_others(seqs):
     out = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, lse=lse, ws=ws)
     check_attention(B, out, lse, what="workspace of the largest step")
     assert torch.equal(out, want)
+
+
+def test_a_buffer_goes_between_attention_and_a_layer_through_init():
+    """The workspaces of serq_paged_attn and of the layers are different things; initialised in between, one buffer is either."""
+    N, K, r = 512, 4096, 32                                        # few channels, one token: the layer's slices meet in its workspace
+    g = torch.Generator(device=DEV).manual_seed(0)
+    pk = serq.pack_weights(torch.randn((N, K), generator=g, device=DEV).bfloat16() * K ** -0.5, None, r,
+                           torch.arange(K, dtype=torch.int32, device=DEV), torch.bfloat16)
+    xq, sc = serq.quantize_act(torch.randn((1, K), generator=g, device=DEV).bfloat16(), pk.s_inv, 8)
+    B = Batch([(1, 9000)], 8, 2, 128, 16, seed=28).fill()
+    own = serq.workspace(1, N, K, r, 8, DEV), serq.paged_attention_workspace(1, 1, 1, 9000, 8, 2, 128, DEV)
+    one = torch.empty(max(w.numel() for w in own), dtype=torch.uint8, device=DEV)
+
+    def layer(ws):
+        return serq.linear(xq, sc, 8, pk.Wq, pk.wscale, 1, N, K, Rp=pk.Rp, r=r, ws=ws).clone()
+
+    def attention(ws):
+        return serq.paged_attention(B.q, *B.args(), 1, 9000, ws=ws)
+
+    want = layer(own[0]), attention(own[1])
+    for _ in range(3):
+        for call, y in zip((layer, attention), want):
+            serq._check("serq_workspace_init", serq.lib().serq_workspace_init(one.data_ptr(), one.numel(), serq._stream()))
+            assert torch.equal(call(one), y) and torch.equal(call(one), y)
