@@ -79,8 +79,9 @@ int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_heads,
  *   s_j = scale * q[t,h,:] . K_j,   out[t,h,:] = sum_j softmax(s)_j V_j,   lse[t,h] = log sum_j exp(s_j),
  * over the positions j with 0 <= j <= p and, where window > 0, j > p - window.  A row that sees no key (p < 0) gives out = 0,
  * lse = -inf.  What a row does not see does not reach its result, whatever it holds, NaN and infinities among it; pages that hold no
- * position that a token of the call sees are not read, and their table entries may be anything.  (NaN or infinite values that a row does see
- * make its result NaN or infinite, which of the two is not defined.)  Page numbers outside 0 .. pages-1 are clamped, lengths past
+ * position that a token of the call sees are not read, and their table entries may be anything.  A key whose score is -inf
+ * weighs nothing, and a row that sees only such keys is as one that sees none.  (Else NaN or infinite values that a row does see make its result NaN or
+ * infinite, which of the two is not defined.)  Page numbers outside 0 .. pages-1 are clamped, lengths past
  * table_width * page_size cut (nothing is read out of bounds; the result is then meaningless).
  *   q, out [tokens, q_heads, dim] in dtype (SERQ_F16 / SERQ_BF16), strides as above; q_heads a multiple of cache->heads.  tokens * q_heads is
  *          at most 2^30, seqs * cache->heads 2^22.

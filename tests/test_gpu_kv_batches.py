@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import kv_oracle as orc
 from paper_2603_08185_amd import binding as serq
 from tests._kv import DEV, Batch, check_attention
 from tests.test_gpu_kv import _bits, _expected_append, _tables
@@ -166,3 +167,35 @@ def test_a_buffer_goes_between_attention_and_a_layer_through_init():
         for call, y in zip((layer, attention), want):
             serq._check("serq_workspace_init", serq.lib().serq_workspace_init(one.data_ptr(), one.numel(), serq._stream()))
             assert torch.equal(call(one), y) and torch.equal(call(one), y)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("seqs", [[(1, 9), (1, 3000), (2, 40)], [(40, 90), (1, 33), (130, 300)]])
+def test_scores_of_minus_infinity_weigh_nothing(seqs, dt):
+    """Keys of -inf in a channel where every query is 1: as if they were not there; a row that sees no other key is as one that sees none."""
+    B = Batch(seqs, 8, 2, 128, 16, dt, seed=29).fill()
+    B.q[..., 0] = 1
+    hidden = []
+    for b, (n, L) in enumerate(B.seqs):
+        j = np.unique(np.concatenate([np.arange(0, L, 3), np.arange(L - n, L - n + n // 2), np.arange(L if b == 0 else 0)]))   # (of the first one: all)
+        page, row = torch.from_numpy(B.table[b, j // 16]).to(DEV), torch.from_numpy(j % 16).to(DEV)
+        B.K[page, row, :, 0] = -float("inf")
+        hidden.append(j)
+    q = B.q.double().cpu().numpy()
+    ws = serq.paged_attention_workspace(B.T, len(B.seqs), B.max_q, B.max_kv, 8, 2, 128, DEV)
+    for use in (None, ws):
+        lse = torch.empty((B.T, 8), device=DEV)
+        out = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, lse=lse, ws=use).double().cpu().numpy()
+        got = lse.double().cpu().numpy()
+        for b, (n, L) in enumerate(B.seqs):
+            for i in range(n):
+                t, keys = B.cu[b] + i, np.setdiff1d(np.arange(L - n + i + 1), hidden[b])
+                if len(keys) == 0:
+                    assert not out[t].any() and np.isneginf(got[t]).all()
+                    continue
+                want, wl, mag, big = orc.attention(q[t:t + 1], B.kv[b][0][keys], B.kv[b][1][keys], 128 ** -0.5, len(keys) - 1)
+                u = 2.0 ** -8 if dt == torch.bfloat16 else 2.0 ** -11
+                esc = 136 * 2.0 ** -24 * big
+                tol = u * np.abs(want) + (2 * u + 2 * esc[..., None] + (32 + L / 16) * 2.0 ** -22) * mag * 1.01 + 2.0 ** -24
+                assert (np.abs(out[t] - want[0]) <= tol[0]).all()
+                assert (np.abs(got[t] - wl[0]) <= esc[0] + (32 + L / 16) * 2.0 ** -22 + 2.0 ** -22 * np.abs(wl[0]) + 2.0 ** -21).all()
