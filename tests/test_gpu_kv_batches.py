@@ -199,3 +199,48 @@ def test_scores_of_minus_infinity_weigh_nothing(seqs, dt):
                 tol = u * np.abs(want) + (2 * u + 2 * esc[..., None] + (32 + L / 16) * 2.0 ** -22) * mag * 1.01 + 2.0 ** -24
                 assert (np.abs(out[t] - want[0]) <= tol[0]).all()
                 assert (np.abs(got[t] - wl[0]) <= esc[0] + (32 + L / 16) * 2.0 ** -22 + 2.0 ** -22 * np.abs(wl[0]) + 2.0 ** -21).all()
+
+
+LONG = [  # new tokens, keys, query heads, key heads, with a workspace
+    (40, 9000, 2, 1, False),                                       # the kernel for many rows, one slice: 141 tiles, whose places are looked up 64 a time
+    (40, 9000, 2, 1, True),
+    (3, 20000, 4, 1, False),                                       # the one for few, a sequence a workgroup
+    (1, 131000, 8, 1, True),                                       # more parts than a wave has lanes
+    (1, 131000, 1, 1, True),                                       # ... and as many as may meet
+    (8, 60000, 4, 1, True),                                        # 32 rows
+]
+
+
+@pytest.mark.parametrize("n,L,Hq,Hkv,sliced", LONG)
+@pytest.mark.parametrize("dt,fp8,D", [(torch.float16, False, 128), (torch.bfloat16, True, 128), (torch.bfloat16, False, 64), (torch.float16, True, 64)])
+def test_attention_long_caches(n, L, Hq, Hkv, sliced, dt, fp8, D):
+    B = Batch([(n, L)], Hq, Hkv, D, 64, dt, fp8, "hnd", seed=30).fill()
+    ws = serq.paged_attention_workspace(n, 1, n, L, Hq, Hkv, D, DEV) if sliced else None
+    for _ in range(2 if sliced else 1):
+        lse = torch.empty((n, Hq), device=DEV)
+        out = serq.paged_attention(B.q, *B.args(), n, L, k_scale=B.k_scale, v_scale=B.v_scale, lse=lse, ws=ws)
+        check_attention(B, out, lse, what=f"{n} tokens over {L} keys")
+
+
+@pytest.mark.parametrize("seqs", [[(1, 5000)], [(1, 700), (1, 33), (0, 0), (1, 1)], [(2, 40), (1, 300), (70, 200), (1, 9)], [(5, 900), (1, 1200)]])
+@pytest.mark.parametrize("Hq,Hkv", [(64, 1), (33, 1), (80, 2), (130, 1)])
+@pytest.mark.parametrize("window,fp8", [(0, False), (50, True)])
+def test_attention_many_query_heads_a_key_head(seqs, Hq, Hkv, window, fp8):
+    B = Batch(seqs, Hq, Hkv, 128, 16, window=window, fp8=fp8, seed=31, extra=1).fill()
+    ws = serq.paged_attention_workspace(B.T, len(B.seqs), B.max_q, B.max_kv, Hq, Hkv, 128, DEV)
+    for use in (None, ws, ws):
+        lse = torch.empty((B.T, Hq), device=DEV)
+        out = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, window=window, k_scale=B.k_scale, v_scale=B.v_scale, lse=lse, ws=use)
+        check_attention(B, out, lse, what=f"{Hq} query heads, {Hkv} key heads")
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+def test_append_every_16_bit_value_passes_unchanged(dt):
+    """Subnormal numbers, signed zeros and infinities among them; NaN stays NaN."""
+    x = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(dt).view(1024, 1, 64).to(DEV)
+    B = Batch([(1024, 1024)], 1, 1, 64, 16, dt)
+    q = serq.kv_append(x, x, x, *B.args())
+    page, row = (torch.from_numpy(a).to(DEV) for a in orc.slots(*orc.positions(B.cu, B.len, 1024), B.table, 16, B.pages))
+    nan = torch.isnan(x)
+    for got in (q, B.K[page, row], B.V[page, row]):
+        assert torch.equal(torch.isnan(got), nan) and torch.equal(_bits(got)[~nan], _bits(x)[~nan])
