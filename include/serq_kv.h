@@ -86,10 +86,12 @@ int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_heads,
  *   q, out [tokens, q_heads, dim] in dtype (SERQ_F16 / SERQ_BF16), strides as above; q_heads a multiple of cache->heads.  tokens * q_heads is
  *          at most 2^30, seqs * cache->heads 2^22.
  *   scale  positive and finite.
- *   max_q, max_kv  upper bounds of n_b and L_b, by which the kernel and the number of slices are chosen (host values; the results do not
- *          depend on them but for the order of fp32 sums).  More tokens or keys than that give SERQ_OK and wrong results, but
+ *   max_q, max_kv  upper bounds of n_b and L_b, by which the kernel and the number of slices are chosen (host values).  Results differ with them as
+ *          sums of another order and weights rounded against another running maximum do, within the errors below.  More tokens or keys than that give SERQ_OK and wrong results, but
  *          nothing is read or written out of bounds.
  *   lse    [tokens, q_heads] fp32, or NULL.
+ * Scores, statistics and sums are fp32.  The softmax' weights are rounded to `dtype` for their product with V, as the matrix instruction takes them; their
+ * sum takes them unrounded.  So a result is within about 2^-8 (bf16) or 2^-11 (fp16) of sum_j softmax_j |V_j|, and rounded once.
  *   workspace  serq_paged_attn_workspace_bytes(...) bytes prepared by serq_workspace_init: where the slices of long caches meet.  What it
  *          returns serves every call of up to as many tokens and sequences, max_q and max_kv, with the same heads: sized once for the largest step.
  *          NULL / 0, or too little, makes the call do without slices, or with fewer.  Left ready for the next call; two calls that share one

@@ -11,9 +11,10 @@
 //            the order 4h .. 4h+3, 8+4h .. 8+4h+3), and V is read by columns in the same order.
 // The 16-byte pieces of a row in LDS are turned by the row's number, so that the lanes that read together meet different banks.
 //
-// 32 query and 8 key heads of 128 channels: a prompt of 8192 tokens 482 us (1.14 PFLOP/s; a large bf16 matrix product reaches 1.4 to 1.6), 512 tokens after
-// 32000 247 us (1.09), 4096 131 us (1.05); E4M3 cache 529, 64 channels 295 (0.93: as many exponentials for half the products).  The clock falls
-// as the matrix units get busier (2.1 to 1.9 GHz): the bound is power.  What carried it (us, before / after, prompt of 8192 unless stated): loads four
+// 32 query and 8 key heads of 128 channels: a prompt of 8192 tokens 482 to 501 us (1.10 to 1.14 PFLOP/s; a large bf16 matrix product reaches 1.4 to 1.6), 512
+// tokens after 32000 247 to 258 us (1.05 to 1.10), 4096 131 to 135 us (1.02 to 1.05); E4M3 cache 529 to 535, 64 channels 295 to 303 (0.91 to 0.93: as many
+// exponentials for half the products).  The clock falls as the matrix units get busier (of 2.4 GHz: 2.0 where they are busy in 47 % of the cycles, with an E4M3
+// cache, 1.78 at 56 %, 512 after 32000, 1.73 at 60 %, the prompt): what the kernel saves in cycles, power takes back in part.  What carried it (us, before / after, prompt of 8192 unless stated): loads four
 // products ahead and the next scores beside the weights 538 / 518, the largest score beside the products with V 528 / 524, the wave
 // at its weights before the one at its products 524 / 506 (512 after 32000: 278 / 258).  Two waves share a SIMD, of two workgroups, so that
 // one is at the exponentials while the other multiplies.
