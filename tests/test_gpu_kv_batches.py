@@ -1,4 +1,5 @@
-"""Batches for the paged cache that a server hands over besides whole ones: a later part of a batch over the whole batch's buffers."""
+"""The paged cache where a call is not the ordinary one: a later part of a batch over the whole batch's buffers, more tokens than were announced, windows, scales and
+weights at the ends of their ranges, a workspace sized for another step, long caches, many query heads a key head."""
 import numpy as np
 import pytest
 import torch
