@@ -20,7 +20,7 @@
 #include <type_traits>
 
 #include "gemm_tile.h"
-#include "serq_device.h"
+#include "quant_codes.h"
 
 namespace serq {
 namespace {
@@ -44,42 +44,6 @@ __device__ __forceinline__ void block_minmax(float& lo, float& hi, float* red) {
   lo = red[0]; hi = red[1];
 #pragma unroll
   for (int i = 1; i < KT / 64; ++i) { lo = fminf(lo, red[2 * i]); hi = fmaxf(hi, red[2 * i + 1]); }
-}
-
-// codes of 8 values: rne(v / sc) + z, clamped to [0, top], re-centred.  t = v * rcp(sc) decides unless it
-// lies within 1.25 * 2^-22 max(|t|, 1) of a half-integer (then, and for tiny scales, the divisions are done).
-template <int ABITS>
-__device__ __forceinline__ void asym_codes8(const float v[8], float sc, float rsc, float z, int c[8]) {
-  constexpr float top = (float)((1 << ABITS) - 1);
-  constexpr float kMagic = 12582912.0f;
-  float r[8], maxd = 0.0f, maxt = 1.0f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float t = v[i] * rsc;
-    r[i] = (t + kMagic) - kMagic;                       // round-half-to-even for |t| < 2^22
-    maxd = fmaxf(maxd, fabsf(t - r[i]));
-    maxt = fmaxf(maxt, fabsf(t));
-  }
-  if (sc < 1e-30f || !(maxt < 4194304.0f) || 0.5f - maxd < 2.98023223876953125e-07f * maxt) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = rintf(v[i] / sc);
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) c[i] = (int)fminf(fmaxf(r[i] + z, 0.0f), top) - (1 << (ABITS - 1));
-}
-
-template <int ABITS>
-__device__ __forceinline__ void store_codes8(const int c[8], void* xq_row, int chunk) {
-  if constexpr (ABITS == 8) {
-    const uint32_t d0 = (c[0] & 0xff) | ((c[1] & 0xff) << 8) | ((c[2] & 0xff) << 16) | ((uint32_t)(c[3] & 0xff) << 24);
-    const uint32_t d1 = (c[4] & 0xff) | ((c[5] & 0xff) << 8) | ((c[6] & 0xff) << 16) | ((uint32_t)(c[7] & 0xff) << 24);
-    ((uint2*)xq_row)[chunk] = make_uint2(d0, d1);
-  } else {
-    uint32_t o = 0;                                     // byte j: code j (low nibble), code 4+j (high nibble)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o |= ((uint32_t)(c[j] & 0xf) | ((uint32_t)(c[4 + j] & 0xf) << 4)) << (8 * j);
-    ((uint32_t*)xq_row)[chunk] = o;
-  }
 }
 
 // KT = threads per row, NC = 16-byte pieces a thread keeps in registers (0: any K, the row is read twice)

@@ -19,7 +19,7 @@
 //                                                   of channel 32*nb + l%32
 // (bytes of blocks past K hold 127).  The compensation matrix is packed like a weight matrix with
 // the rank index in the place of the input channel.
-#include "serq_device.h"
+#include "quant_codes.h"
 
 namespace serq {
 namespace {
@@ -29,14 +29,6 @@ constexpr int kMaxGridY = 65535;                      // where a grid's y dimens
 inline unsigned blocks_for(size_t n) { return (unsigned)((n + kT - 1) / kT); }
 inline int ok() { return hipGetLastError() == hipSuccess ? SERQ_OK : SERQ_EHIP; }
 
-// shared exponent byte of a block whose largest magnitude is amax
-__device__ __forceinline__ int mx_exponent(float amax) {
-  if (!(amax > 0.0f)) return 127;
-  const int ef = (int)((__float_as_uint(amax) >> 23) & 0xffu);      // 0 for subnormals: clipped below anyway
-  int se = ef - 127 - 2;
-  se = se < -127 ? -127 : se;
-  return se + 127;
-}
 // v * 2^-(E-127): exact unless the result is subnormal, and then it is far below the smallest midpoint
 __device__ __forceinline__ float mx_scale_down(float v, int E) {
   return ldexpf(v, 127 - E);
@@ -52,23 +44,6 @@ __device__ __forceinline__ float e2m1_value(uint32_t code) {
   // 0, .5, 1, 1.5, 2, 3, 4, 6
   const float v = i < 2 ? 0.5f * (float)i : ldexpf(1.0f + 0.5f * (float)(i & 1u), (int)(i >> 1) - 1);
   return (code & 8u) ? -v : v;
-}
-// The same eight codes from the part's own conversion instruction (two fp32 values divided by the
-// power of two in the scale operand's exponent field, rounded to nearest even on the E2M1 grid and
-// saturated, packed into one byte: low nibble first operand, high nibble second), already in the
-// interleaved nibble layout.  The instruction keeps the sign of a value that rounds to zero; codes are
-// canonical here (zero has sign 0), so the sign bit of every nibble without magnitude bits is cleared.
-// Checked against the comparison form above on a million random pairs, every tie, saturation and the
-// ends of the exponent range: identical.
-__device__ __forceinline__ uint32_t mx_codes8(const float v[8], int E) {
-  const float sc = __uint_as_float((uint32_t)E << 23);
-  uint32_t d = 0;
-  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, v[0], v[4], sc, 0);
-  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, v[1], v[5], sc, 1);
-  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, v[2], v[6], sc, 2);
-  d = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(d, v[3], v[7], sc, 3);
-  const uint32_t nz = ((d & 0x77777777u) + 0x77777777u) & 0x88888888u;   // bit 3 of a nibble: its magnitude is not zero
-  return d & (0x77777777u | nz);
 }
 // eight codes (channels k0 .. k0+7) -> one dword in the interleaved nibble layout
 __device__ __forceinline__ uint32_t pack8(const uint32_t c[8]) {

@@ -15,72 +15,10 @@
 // down projection, quantised where it is made instead of being stored in 16 bits and read back;
 // Sec. 3.2, the decoder-layer flow of Fig. 2(b)).  The product is formed in fp32 (hardware exp2 and
 // reciprocal, an ulp each) and never rounded to the storage type.
-#include "serq_device.h"
+#include "quant_codes.h"
 
 namespace serq {
 namespace {
-
-__device__ __forceinline__ float absmax8(const float v[8], float m) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));
-  return m;
-}
-
-// Codes of 8 flattened values, bit-identical to clip(rne(v / sc)) in IEEE fp32, at the price of
-// a multiplication per value.  t = v * rcp(sc) is within 2^-22 |t| of the correctly rounded
-// quotient (one ulp from the reciprocal, half an ulp from the product, half an ulp from the
-// quotient's own rounding), so the two round to the same integer unless t lies within that distance
-// of a half-integer; only then (the ties of synthetic inputs, and about one piece in a hundred
-// otherwise) are the divisions carried out.  The margin used is 1.25 * 2^-22 max(|t|, 1) over the piece.
-// A token whose scale is tiny (below 1e-30, a wave-uniform test: the reciprocal of a subnormal scale is
-// not finite, and neither estimate above holds near the bottom of the exponent range) always takes the
-// divisions.
-// (The bookkeeping of this check -- four VALU operations per value -- costs about a tenth of the
-// kernel's time; the fallback itself is too rare to show.)
-// Clamping before rounding equals rounding before clamping for integer bounds, and adding
-// 1.5 * 2^23 rounds to nearest-even and leaves the two's-complement code in the low mantissa bits.
-template <int ABITS>
-__device__ __forceinline__ void codes8(const float v[8], float sc, float rsc, uint32_t u[8]) {
-  constexpr float q = (float)((1 << (ABITS - 1)) - 1);
-  constexpr float kMagic = 12582912.0f;
-  float maxd = 0.0f, maxt = 1.0f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float tc = __builtin_amdgcn_fmed3f(v[i] * rsc, -q, q);
-    const float uf = tc + kMagic;
-    u[i] = __float_as_uint(uf);
-    maxd = fmaxf(maxd, fabsf(tc - (uf - kMagic)));
-    maxt = fmaxf(maxt, fabsf(tc));
-  }
-  if (sc < 1e-30f || 0.5f - maxd < 2.98023223876953125e-07f * maxt) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float t = rintf(v[i] / sc);          // IEEE division, then round-half-to-even
-      t = fminf(fmaxf(t, -q), q);
-      u[i] = __float_as_uint(t + kMagic);
-    }
-  }
-}
-
-template <int ABITS>
-__device__ __forceinline__ void quant_store8(const float v[8], float sc, void* xq_row, int chunk) {
-  const float rsc = __builtin_amdgcn_rcpf(sc);
-  uint32_t u[8];
-  codes8<ABITS>(v, sc, rsc, u);
-  if constexpr (ABITS == 8) {
-    // low bytes of u[0..3] and u[4..7]
-    const uint32_t d0 = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u) | __builtin_amdgcn_perm(u[3], u[2], 0x04000c0cu);
-    const uint32_t d1 = __builtin_amdgcn_perm(u[5], u[4], 0x0c0c0400u) | __builtin_amdgcn_perm(u[7], u[6], 0x04000c0cu);
-    ((uint2*)xq_row)[chunk] = make_uint2(d0, d1);
-  } else {
-    // byte j = code j in the low nibble, code 4+j in the high nibble
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = (u[4 + j] << 4) | (u[j] & 0xfu);
-    ((uint32_t*)xq_row)[chunk] =
-        __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0400u) | __builtin_amdgcn_perm(w[3], w[2], 0x04000c0cu);
-  }
-}
 
 template <int KT>
 __device__ __forceinline__ float block_max(float m, float* red) {
