@@ -8,7 +8,9 @@
  * declared further down: the compensation matrix on the INT4 grid
  * (serq_pack_lowrank_q4), the whole layer in MXFP4 (serq_mx_*), and the
  * quantisers fused into the producer of the down projection's input
- * (serq_swiglu_quantize_act, serq_mx_swiglu_quantize_act).
+ * (serq_swiglu_quantize_act, serq_mx_swiglu_quantize_act) and into the residual
+ * sum and norm before the other projections (serq_rmsnorm_quantize_act,
+ * serq_rmsnorm_quantize_act_asym, serq_mx_rmsnorm_quantize_act).
  *
  * Conventions for every entry point
  *   - Every data pointer is a DEVICE pointer owned by the caller, 16-byte
@@ -350,6 +352,32 @@ int serq_g128_linear(const void* Xq, const float* scale, const int32_t* zero, in
                      const void* Wq, const void* gscale, const float* wsum,
                      int s_begin, int r, const void* Rp, int r_dtype,
                      int64_t M, int64_t N, int64_t K, void* Y, int y_dtype, int64_t ldy, int flags, void* stream);
+
+/*
+ * ---- The quantisers fused into what makes the input of the q/k/v and the gate/up projections -----------------
+ * Residual sum, root-mean-square norm, flattening and quantisation in one pass (Sec. 3.2, the decoder-layer flow of Fig. 2(b): the
+ * flattening is merged into the norm before it):
+ *   h[m,k]  = X[m,k] + residual[m,k], an fp32 sum rounded to x_dtype (no residual: h = X)
+ *   rstd[m] = 1 / sqrt(mean_k h[m,k]^2 + eps), formed in 64 bits, rounded to fp32, at most the largest finite number (0 where the root is 0)
+ *   u[m,k]  = h[m,k] * gain[k], one fp32 multiply
+ * gain [K] fp32 holds the norm's weight times the flattening factor s_inv, in permuted order; NULL: all ones.  The normalised row is
+ * u rstd.  Symmetric and asymmetric codes are those that serq_quantize_act and serq_quantize_act_asym give for u, and
+ *   scale_out[m] = fl(scale_u * rstd)  (1.0 for a token whose u are all zero);
+ * MXFP4 codes and exponents are those that serq_mx_quantize_act gives for fl(u * rstd).
+ *   X, residual [M,K] in x_dtype, row strides ldx, ldr (multiples of 8).  residual may be NULL (ldr, ldh ignored, h_out NULL).
+ *   h_out [M,K] in x_dtype, row stride ldh: the sum, which the next layer's residual is.  It may be X or residual itself (same stride), but
+ *         must not overlap them otherwise.
+ *   eps   finite, not negative.
+ * The sums of squares are exact enough for every output to be the same whatever the row's split (a sum of fp32 squares rounds in 64 bits).
+ * M up to 2^30.  Everything else as the quantisers named.
+ */
+int serq_rmsnorm_quantize_act(const void* X, const void* residual, int x_dtype, const float* gain, float eps, int64_t M, int64_t K,
+                              int64_t ldx, int64_t ldr, void* h_out, int64_t ldh, int abits, void* Xq_out, float* scale_out, void* stream);
+int serq_rmsnorm_quantize_act_asym(const void* X, const void* residual, int x_dtype, const float* gain, float eps, int64_t M, int64_t K,
+                                   int64_t ldx, int64_t ldr, void* h_out, int64_t ldh, int abits, void* Xq_out, float* scale_out,
+                                   int32_t* zero_out, void* stream);
+int serq_mx_rmsnorm_quantize_act(const void* X, const void* residual, int x_dtype, const float* gain, float eps, int64_t M, int64_t K,
+                                 int64_t ldx, int64_t ldr, void* h_out, int64_t ldh, void* Xq_out, uint8_t* xscale_out, void* stream);
 
 #ifdef __cplusplus
 }

@@ -454,6 +454,34 @@ def mx_swiglu_quantize_act(gate, up, s_inv):
     return mx_quantize_act(swiglu(gate, up), s_inv)
 
 
+def rmsnorm_rows(h: np.ndarray, gain, eps: float):
+    """(u, rstd) of rows h (fp32 values of the stored sum): u = fl(h * gain), rstd = 1 / sqrt(mean h^2 + eps) formed in fp64, rounded to
+    fp32 and kept finite; 0 where the root is 0."""
+    h = np.asarray(h, F32)
+    ms = (h.astype(np.float64) ** 2).sum(axis=1) / h.shape[1] + np.float64(F32(eps))
+    with np.errstate(divide="ignore", over="ignore"):
+        rstd = np.where(ms > 0, 1.0 / np.sqrt(ms), 0.0).astype(F32)
+    return flatten(h, gain), np.minimum(rstd, np.finfo(F32).max)
+
+
+def rmsnorm_quantize_act(h, gain, eps: float, abits: int):
+    """Codes of u, and the token's scale times rstd (1.0 for a token whose u are all zero)."""
+    u, rstd = rmsnorm_rows(h, gain, eps)
+    Xq, scale = quantize_act(u, None, abits)
+    return Xq, np.where(np.abs(u).max(axis=1) > 0, (scale * rstd).astype(F32), F32(1.0))
+
+
+def rmsnorm_quantize_act_asym(h, gain, eps: float, abits: int):
+    u, rstd = rmsnorm_rows(h, gain, eps)
+    Xq, scale, zero = quantize_act_asym(u, None, abits)
+    return Xq, np.where(np.abs(u).max(axis=1) > 0, (scale * rstd).astype(F32), F32(1.0)), zero
+
+
+def mx_rmsnorm_quantize_act(h, gain, eps: float):
+    u, rstd = rmsnorm_rows(h, gain, eps)
+    return mx_quantize_act((u * rstd[:, None]).astype(F32), None)
+
+
 def linear_f32(Xq, scale, Wq, wscale, R=None, s_begin: int = 0, acc=None) -> np.ndarray:
     """The same formula evaluated in fp32 in the stated order (documents fp32's share of the tolerance)."""
     if acc is None:

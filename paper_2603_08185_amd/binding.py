@@ -63,6 +63,9 @@ SIGNATURES = {
     "serq_g128_pack_weights": (_i, [_vp, _i, _vp, _vp, _i64, _i64, _i, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp]),
     "serq_g128_unpack_scales": (_i, [_vp, _i64, _i64, _vp, _vp]),
     "serq_g128_linear": (_i, [_vp, _vp, _vp, _i, _vp, _vp, _vp, _i, _i, _vp, _i, _i64, _i64, _i64, _vp, _i, _i64, _i, _vp]),
+    "serq_rmsnorm_quantize_act": (_i, [_vp, _vp, _i, _vp, C.c_float, _i64, _i64, _i64, _i64, _vp, _i64, _i, _vp, _vp, _vp]),
+    "serq_rmsnorm_quantize_act_asym": (_i, [_vp, _vp, _i, _vp, C.c_float, _i64, _i64, _i64, _i64, _vp, _i64, _i, _vp, _vp, _vp, _vp]),
+    "serq_mx_rmsnorm_quantize_act": (_i, [_vp, _vp, _i, _vp, C.c_float, _i64, _i64, _i64, _i64, _vp, _i64, _vp, _vp, _vp]),
     "serq_fp6_weight_bytes": (_sz, [_i64, _i64]),
     "serq_fp6_act_bytes": (_sz, [_i64, _i64]),
     "serq_fp6_pack_weights": (_i, [_vp, _i64, _i64, _vp, _vp]),
@@ -86,6 +89,8 @@ _FAST = ["serq_quantize_act", "serq_swiglu_quantize_act", "serq_mx_quantize_act"
          "serq_quantize_act_asym", "serq_linear", "serq_mx_linear", "serq_g128_linear"]
 # ... and in that of its bind_kv()
 _FAST_KV = ["serq_kv_append", "serq_paged_attn"]
+# ... and in that of its bind_norm()
+_FAST_NORM = ["serq_rmsnorm_quantize_act", "serq_rmsnorm_quantize_act_asym", "serq_mx_rmsnorm_quantize_act"]
 
 
 class SerqError(RuntimeError):
@@ -125,6 +130,7 @@ def _load_fastcall(L: C.CDLL) -> None:
         return
     mod.bind(*(C.cast(getattr(L, name), C.c_void_p).value for name in _FAST))
     mod.bind_kv(*(C.cast(getattr(L, name), C.c_void_p).value for name in _FAST_KV))
+    mod.bind_norm(*(C.cast(getattr(L, name), C.c_void_p).value for name in _FAST_NORM))
     _fast = mod
 
 
@@ -608,6 +614,98 @@ def g128_linear(Xq: torch.Tensor, scale: torch.Tensor, zero: Optional[torch.Tens
                                 _ptr(Rp), _DT[r_dtype], M, N, K, _ptr(Y), _DT[Y.dtype], Y.stride(0), flags_, _stream())
     _check("serq_g128_linear", rc)
     return Y
+
+
+# ---- the quantisers fused into the residual sum and the norm ---------------------------------------------------
+def _norm_rows(X, gain, residual, h):
+    """Checks of rmsnorm_quantize_act and its forms; returns the arguments that describe the rows, and h."""
+    _rows(X, "X")
+    if X.dtype not in _DT:
+        raise ValueError("X must be float32, float16 or bfloat16")
+    M, K = X.shape
+    if gain is not None and (not gain.is_cuda or gain.dtype != torch.float32 or gain.shape != (K,) or not gain.is_contiguous()):
+        raise ValueError("gain must be fp32 [K] in device memory")
+    if residual is None:
+        if h is not None:
+            raise ValueError("without a residual the sum is X itself: no h")
+        return (M, K, X.stride(0) if M > 0 else K, 0), None
+    if h is None:
+        h = torch.empty((M, K), dtype=X.dtype, device=X.device)
+    for t, what in ((residual, "residual"), (h, "h")):
+        _rows(t, what)
+        if t.shape != X.shape or t.dtype != X.dtype:
+            raise ValueError(f"{what} must agree with X in shape and dtype")
+    return (M, K, X.stride(0) if M > 0 else K, residual.stride(0) if M > 0 else K), h
+
+
+def _buffer(t: Optional[torch.Tensor], n: int, what: str, dtype: torch.dtype, device) -> torch.Tensor:
+    """A caller's output buffer of at least n elements, or a new one."""
+    if t is None:
+        return torch.empty(max(n, 16), dtype=dtype, device=device)
+    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{what} must be a contiguous {dtype} buffer of at least {n} elements in device memory")
+    return t
+
+
+def rmsnorm_quantize_act(X: torch.Tensor, gain: Optional[torch.Tensor], eps: float, abits: int, residual: Optional[torch.Tensor] = None,
+                         h: Optional[torch.Tensor] = None, Xq: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
+    """serq_rmsnorm_quantize_act: quantize_act of the normalised sum X + residual times gain; returns (Xq packed uint8 blob, scale fp32 [M],
+    the sum: h, or X where there is no residual)."""
+    if Xq is not None and scale is not None and (residual is None or h is not None):
+        rc = (_fast or _native()).rmsnorm_quantize_act(X, gain, eps, abits, residual, h, Xq, scale)
+        if rc == 0:
+            return Xq, scale, X if h is None else h
+        if rc is not None:
+            raise SerqError("serq_rmsnorm_quantize_act", rc)
+    (M, K, ldx, ldr), h = _norm_rows(X, gain, residual, h)
+    L = lib()
+    Xq = _buffer(Xq, L.serq_packed_act_bytes(M, K, abits), "Xq", torch.uint8, X.device)
+    scale = _buffer(scale, M, "scale", torch.float32, X.device)[:M]
+    rc = L.serq_rmsnorm_quantize_act(_ptr(X), _ptr(residual), _DT[X.dtype], _ptr(gain), eps, M, K, ldx, ldr, _ptr(h),
+                                     h.stride(0) if h is not None and M > 0 else K, abits, _ptr(Xq), _ptr(scale), _stream())
+    _check("serq_rmsnorm_quantize_act", rc)
+    return Xq, scale, X if h is None else h
+
+
+def rmsnorm_quantize_act_asym(X: torch.Tensor, gain: Optional[torch.Tensor], eps: float, abits: int, residual: Optional[torch.Tensor] = None,
+                              h: Optional[torch.Tensor] = None, Xq: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                              zero: Optional[torch.Tensor] = None):
+    """serq_rmsnorm_quantize_act_asym: quantize_act_asym of the normalised sum; returns (Xq packed uint8 blob, scale fp32 [M], zero int32
+    [M], the sum)."""
+    if Xq is not None and scale is not None and zero is not None and (residual is None or h is not None):
+        rc = (_fast or _native()).rmsnorm_quantize_act_asym(X, gain, eps, abits, residual, h, Xq, scale, zero)
+        if rc == 0:
+            return Xq, scale, zero, X if h is None else h
+        if rc is not None:
+            raise SerqError("serq_rmsnorm_quantize_act_asym", rc)
+    (M, K, ldx, ldr), h = _norm_rows(X, gain, residual, h)
+    L = lib()
+    Xq = _buffer(Xq, L.serq_packed_act_bytes(M, K, abits), "Xq", torch.uint8, X.device)
+    scale = _buffer(scale, M, "scale", torch.float32, X.device)[:M]
+    zero = _buffer(zero, M, "zero", torch.int32, X.device)[:M]
+    rc = L.serq_rmsnorm_quantize_act_asym(_ptr(X), _ptr(residual), _DT[X.dtype], _ptr(gain), eps, M, K, ldx, ldr, _ptr(h),
+                                          h.stride(0) if h is not None and M > 0 else K, abits, _ptr(Xq), _ptr(scale), _ptr(zero), _stream())
+    _check("serq_rmsnorm_quantize_act_asym", rc)
+    return Xq, scale, zero, X if h is None else h
+
+
+def mx_rmsnorm_quantize_act(X: torch.Tensor, gain: Optional[torch.Tensor], eps: float, residual: Optional[torch.Tensor] = None,
+                            h: Optional[torch.Tensor] = None, Xq: Optional[torch.Tensor] = None, xsc: Optional[torch.Tensor] = None):
+    """serq_mx_rmsnorm_quantize_act: mx_quantize_act of the normalised sum; returns (codes blob, block-scale blob, the sum)."""
+    if Xq is not None and xsc is not None and (residual is None or h is not None):
+        rc = (_fast or _native()).mx_rmsnorm_quantize_act(X, gain, eps, residual, h, Xq, xsc)
+        if rc == 0:
+            return Xq, xsc, X if h is None else h
+        if rc is not None:
+            raise SerqError("serq_mx_rmsnorm_quantize_act", rc)
+    (M, K, ldx, ldr), h = _norm_rows(X, gain, residual, h)
+    L = lib()
+    Xq = _buffer(Xq, L.serq_packed_act_bytes(M, K, 4), "Xq", torch.uint8, X.device)
+    xsc = _buffer(xsc, L.serq_mx_act_scale_bytes(M, K), "xsc", torch.uint8, X.device)
+    rc = L.serq_mx_rmsnorm_quantize_act(_ptr(X), _ptr(residual), _DT[X.dtype], _ptr(gain), eps, M, K, ldx, ldr, _ptr(h),
+                                        h.stride(0) if h is not None and M > 0 else K, _ptr(Xq), _ptr(xsc), _stream())
+    _check("serq_mx_rmsnorm_quantize_act", rc)
+    return Xq, xsc, X if h is None else h
 
 
 # ---- experiment: W4A4 integer sums on the FP6 form of the scaled matrix instruction -----------------------

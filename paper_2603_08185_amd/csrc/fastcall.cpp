@@ -29,6 +29,9 @@ decltype(&serq_mx_linear) f_mx_linear;
 decltype(&serq_g128_linear) f_g128_linear;
 decltype(&serq_kv_append) f_kv_append;
 decltype(&serq_paged_attn) f_paged_attn;
+decltype(&serq_rmsnorm_quantize_act) f_rmsnorm_quantize_act;
+decltype(&serq_rmsnorm_quantize_act_asym) f_rmsnorm_quantize_act_asym;
+decltype(&serq_mx_rmsnorm_quantize_act) f_mx_rmsnorm_quantize_act;
 
 // Arguments of one call; `ok` falls once one of them is not the plain thing.
 struct Args {
@@ -63,6 +66,10 @@ struct Args {
       case at::kBFloat16: return SERQ_BF16;
       default: ok = false; return 0;
     }
+  }
+  float real(int i) {                                  // of a float
+    if (!PyFloat_CheckExact(a[i])) { ok = false; return 0.0f; }
+    return (float)PyFloat_AS_DOUBLE(a[i]);
   }
   // [M, K] activations with unit inner stride
   struct Rows { void* p; int dt; int64_t M, K, ld; };
@@ -286,6 +293,71 @@ Cache cache(Args& x, int i, int s, const Heads& q) {
          B <= 1 ? std::max(tb->stride(0), tb->size(1)) : tb->stride(0), q.T, (int32_t)tb->size(1), (int32_t)B};
   return r;
 }
+// ---- the quantisers fused into the residual sum and the norm: types and sizes of all tensors are checked here too ---------------------
+// X, gain, eps from argument 0 on; residual, h from argument i on
+struct NormIn { Args::Rows x, r, h; const float* gain; float eps; };
+NormIn norm_in(Args& x, int i) {
+  NormIn n{};
+  n.x = x.rows(0);
+  n.gain = scales(x, 1, n.x.K);
+  n.eps = x.real(2);
+  if (!x.ok) return n;
+  if (x.a[i] != Py_None) {
+    n.r = x.rows(i);
+    n.h = x.rows(i + 1);
+    x.alike(n.x, n.r);
+    x.alike(n.x, n.h);
+  } else if (x.a[i + 1] != Py_None) {
+    x.ok = false;
+  }
+  return n;
+}
+// a contiguous buffer of at least n elements
+void* buffer(Args& x, int i, at::ScalarType type, int64_t n) {
+  const at::Tensor* t = x.ok ? x.tensor(i) : nullptr;
+  if (!t || !t->is_cuda() || t->scalar_type() != type || !t->is_contiguous() || t->numel() < n) { x.ok = false; return nullptr; }
+  return t->data_ptr();
+}
+
+// X, gain, eps, abits, residual, h, Xq, scale
+PyObject* rmsnorm_quantize_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(a, n, 8, [](Args& x) {
+    const NormIn r = norm_in(x, 4);
+    const int abits = x.integer32(3);
+    void* xq = buffer(x, 6, at::kByte, r.x.M * r.x.K * abits / 8);
+    float* sc = (float*)buffer(x, 7, at::kFloat, r.x.M);
+    return [=](void* st) {
+      return f_rmsnorm_quantize_act(r.x.p, r.r.p, r.x.dt, r.gain, r.eps, r.x.M, r.x.K, r.x.ld, r.r.ld, r.h.p, r.h.ld, abits, xq, sc, st);
+    };
+  });
+}
+
+// X, gain, eps, abits, residual, h, Xq, scale, zero
+PyObject* rmsnorm_quantize_act_asym(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(a, n, 9, [](Args& x) {
+    const NormIn r = norm_in(x, 4);
+    const int abits = x.integer32(3);
+    void* xq = buffer(x, 6, at::kByte, r.x.M * r.x.K * abits / 8);
+    float* sc = (float*)buffer(x, 7, at::kFloat, r.x.M);
+    int32_t* z = (int32_t*)buffer(x, 8, at::kInt, r.x.M);
+    return [=](void* st) {
+      return f_rmsnorm_quantize_act_asym(r.x.p, r.r.p, r.x.dt, r.gain, r.eps, r.x.M, r.x.K, r.x.ld, r.r.ld, r.h.p, r.h.ld, abits, xq, sc, z, st);
+    };
+  });
+}
+
+// X, gain, eps, residual, h, Xq, xsc
+PyObject* mx_rmsnorm_quantize_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(a, n, 7, [](Args& x) {
+    const NormIn r = norm_in(x, 3);
+    void* xq = buffer(x, 5, at::kByte, r.x.M * r.x.K / 2);
+    uint8_t* sc = (uint8_t*)buffer(x, 6, at::kByte, (r.x.K + 255) / 256 * ((r.x.M + 1) & ~(int64_t)1) * 8);
+    return [=](void* st) {
+      return f_mx_rmsnorm_quantize_act(r.x.p, r.r.p, r.x.dt, r.gain, r.eps, r.x.M, r.x.K, r.x.ld, r.r.ld, r.h.p, r.h.ld, xq, sc, st);
+    };
+  });
+}
+
 bool same_rows(const Heads& a, const Heads& b) { return a.T == b.T && a.D == b.D && a.dt == b.dt; }
 
 // q, k, v, K, V, table, cu_q, kv_len, cos, sin, interleaved, positions, k_scale, v_scale, q_out
@@ -384,12 +456,17 @@ PyObject* bind_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void** const slots[] = {(void**)&f_kv_append, (void**)&f_paged_attn};
   return bind_slots(slots, sizeof(slots) / sizeof(slots[0]), a, n);
 }
+PyObject* bind_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void** const slots[] = {(void**)&f_rmsnorm_quantize_act, (void**)&f_rmsnorm_quantize_act_asym, (void**)&f_mx_rmsnorm_quantize_act};
+  return bind_slots(slots, sizeof(slots) / sizeof(slots[0]), a, n);
+}
 
 #define SERQ_FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SERQ_FAST(bind), SERQ_FAST(quantize_act), SERQ_FAST(swiglu_quantize_act), SERQ_FAST(mx_quantize_act),
                          SERQ_FAST(mx_swiglu_quantize_act), SERQ_FAST(quantize_act_asym), SERQ_FAST(linear),
                          SERQ_FAST(mx_linear), SERQ_FAST(g128_linear), SERQ_FAST(bind_kv), SERQ_FAST(kv_append),
-                         SERQ_FAST(paged_attention), {nullptr, nullptr, 0, nullptr}};
+                         SERQ_FAST(paged_attention), SERQ_FAST(bind_norm), SERQ_FAST(rmsnorm_quantize_act),
+                         SERQ_FAST(rmsnorm_quantize_act_asym), SERQ_FAST(mx_rmsnorm_quantize_act), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
