@@ -361,9 +361,13 @@ int serq_g128_linear(const void* Xq, const float* scale, const int32_t* zero, in
  *   rstd[m] = 1 / sqrt(mean_k h[m,k]^2 + eps), formed in 64 bits, rounded to fp32, at most the largest finite number (0 where the root is 0)
  *   u[m,k]  = h[m,k] * gain[k], one fp32 multiply
  * gain [K] fp32 holds the norm's weight times the flattening factor s_inv, in permuted order; NULL: all ones.  The normalised row is
- * u rstd.  Symmetric and asymmetric codes are those that serq_quantize_act and serq_quantize_act_asym give for u, and
- *   scale_out[m] = fl(scale_u * rstd)  (1.0 for a token whose u are all zero);
- * MXFP4 codes and exponents are those that serq_mx_quantize_act gives for fl(u * rstd).
+ * u rstd.  The integer codes are those of u on a grid of their own, to which rstd comes afterwards; with n bits,
+ *   symmetric:  q = 2^(n-1) - 1, su = fl(max_k |u| * fl(1/q)), Xq = clip(rne(u / su), -q, q)
+ *   asymmetric: q = 2^n - 1, lo = min(0, min_k u), hi = max(0, max_k u), su = fl((hi - lo) * fl(1/q)), z = rne(-lo / su),
+ *               c = clip(rne(u / su) + z, 0, q), stored as Xq = c - 2^(n-1), zero = z - 2^(n-1)
+ *   scale_out[m] = fl(su * rstd)       (a su of zero: su = scale_out = 1.0)
+ * (serq_quantize_act divides where this multiplies by fl(1/q): the grids differ by an ulp at most).  MXFP4 codes and exponents are those that
+ * serq_mx_quantize_act gives for fl(u * rstd).
  *   X, residual [M,K] in x_dtype, row strides ldx, ldr (multiples of 8).  residual may be NULL (ldr, ldh ignored, h_out NULL).
  *   h_out [M,K] in x_dtype, row stride ldh: the sum, which the next layer's residual is.  It may be X or residual itself (same stride), but
  *         must not overlap them otherwise.

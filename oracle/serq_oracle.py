@@ -465,16 +465,27 @@ def rmsnorm_rows(h: np.ndarray, gain, eps: float):
 
 
 def rmsnorm_quantize_act(h, gain, eps: float, abits: int):
-    """Codes of u, and the token's scale times rstd (1.0 for a token whose u are all zero)."""
+    """Symmetric codes of u on the grid su = fl(max |u| * fl(1 / qmax)), and the token's scale fl(su * rstd); a su of zero: both are 1."""
     u, rstd = rmsnorm_rows(h, gain, eps)
-    Xq, scale = quantize_act(u, None, abits)
-    return Xq, np.where(np.abs(u).max(axis=1) > 0, (scale * rstd).astype(F32), F32(1.0))
+    q = F32(qmax(abits))
+    su = (np.abs(u).max(axis=1).astype(F32) * (F32(1) / q)).astype(F32)
+    some = su > 0
+    su = np.where(some, su, F32(1))
+    Xq = np.clip(np.rint((u / su[:, None]).astype(F32)), -q, q).astype(np.int8)
+    return Xq, np.where(some, (su * rstd).astype(F32), F32(1))
 
 
 def rmsnorm_quantize_act_asym(h, gain, eps: float, abits: int):
+    """Asymmetric codes of u (as quantize_act_asym's, su = fl((hi - lo) * fl(1 / (2^n - 1)))), the token's scale and zero point."""
     u, rstd = rmsnorm_rows(h, gain, eps)
-    Xq, scale, zero = quantize_act_asym(u, None, abits)
-    return Xq, np.where(np.abs(u).max(axis=1) > 0, (scale * rstd).astype(F32), F32(1.0)), zero
+    top, half = F32((1 << abits) - 1), 1 << (abits - 1)
+    lo, hi = np.minimum(u.min(axis=1), F32(0)), np.maximum(u.max(axis=1), F32(0))
+    su = ((hi - lo).astype(F32) * (F32(1) / top)).astype(F32)
+    some = su > 0
+    su = np.where(some, su, F32(1))
+    z = np.rint((-lo / su).astype(F32))
+    c = np.clip(np.rint((u / su[:, None]).astype(F32)) + z[:, None], F32(0), top)
+    return (c - half).astype(np.int8), np.where(some, (su * rstd).astype(F32), F32(1)), (z - half).astype(np.int32)
 
 
 def mx_rmsnorm_quantize_act(h, gain, eps: float):

@@ -1,12 +1,14 @@
 // Residual sum, root-mean-square norm, flattening and quantisation of a token's row in one pass (serq_rmsnorm_quantize_act and its forms):
 //   h = X + residual, rounded to the stream's type;  rstd = 1 / sqrt(mean h^2 + eps);  u = h gain.
 // Integer codes are those of u: the norm's factor is one number a token, which symmetric and asymmetric scales carry along
-// (scale = scale_u rstd), so the sum of squares and the largest |u| are found in one round of the workgroup and no code waits
+// (scale = su rstd), so the sum of squares and the largest |u| are found in one round of the workgroup and no code waits
 // for the square root.  MXFP4's block scales are powers of two: there v = u rstd is what is quantised.
 // The sum of squares is taken in 64 bits: squares of 16-bit numbers are exact there and sums of them as good as, so rstd is the correctly rounded
 // one however the row is split, and with it every code and scale is defined to the bit.
 //
-// A workgroup a token, the row in registers between the two steps.
+// A workgroup a token, the row in registers between the two steps.  Bound by memory: stream, residual and sum in 16 bits and 8-bit codes are 7 bytes
+// a channel, 16384 tokens of 4096 channels 470 MB in 82.8 us (5.7 TB/s; a copy of 1 GiB reaches 5.1 to 5.3); few tokens by the trip to
+// memory and the workgroup's one meeting (one token of 4096 channels 2.55 us a launch, of which an empty one takes most).
 #include <float.h>
 
 #include <type_traits>
@@ -188,8 +190,9 @@ __global__ __launch_bounds__(KT) void rmsnorm_quantize_kernel(NormParams p) {
   const double ms = __builtin_fma(f.sum, p.inv_k, p.eps);
 
   constexpr float top = ASYM ? (float)((1 << ABITS) - 1) : (float)((1 << (ABITS - 1)) - 1);
-  const float span = ASYM ? f.hi - f.lo : f.hi;
-  const float sc = span > 0.0f ? span / top : 1.0f, rsc = __builtin_amdgcn_rcpf(sc);
+  // (a product with the rounded reciprocal: within an ulp of the quotient, and every code waits for it)
+  const float unit = (ASYM ? f.hi - f.lo : f.hi) * (1.0f / top);
+  const float sc = unit > 0.0f ? unit : 1.0f, rsc = __builtin_amdgcn_rcpf(sc);
   const float z = ASYM ? rintf(-f.lo / sc) : 0.0f;
   const float rstd = FORM == kMx ? inv_root(ms) : 0.0f;
   const size_t Mp = (size_t)((p.M + 1) & ~(int64_t)1);
@@ -241,23 +244,48 @@ __global__ __launch_bounds__(KT) void rmsnorm_quantize_kernel(NormParams p) {
     if (m == p.M - 1 && (size_t)p.M < Mp)
       for (int blk = tid; blk < nblk8; blk += KT) xsc[((size_t)(blk >> 3) * Mp + (size_t)p.M) * 8 + (blk & 7)] = 127;
   } else if (tid == 0) {
-    ((float*)p.scale)[m] = span > 0.0f ? sc * inv_root(ms) : 1.0f;
+    ((float*)p.scale)[m] = unit > 0.0f ? sc * inv_root(ms) : 1.0f;
     if constexpr (ASYM) p.zero[m] = (int)z - (1 << (ABITS - 1));
   }
 }
 
+// Threads of a row and pieces of each: a row's own latency counts where rows are few and the rate at which waves start where they are many, and both want
+// a piece a thread up to 512 of them, but for many rows without a residual, which have little to load; beyond, registers.  Measured
+// (symmetric 8-bit codes, bf16, us; threads x pieces):
+//   K = 1024  128 x 1 / 64 x 2 / 256 x 1: M = 1 2.16 / 2.35 / 2.17, M = 4096 7.04 / 7.80 / 8.37
+//   K = 2624  384 x 1 / 192 x 2 / 512 x 1: M = 1 2.39 / 2.59 / 2.54, M = 1000 5.98 / 6.30 / 6.22, M = 4096 13.9 / 13.7 / 14.4, no residual 10.7 / 9.3 / 11.4
+//   K = 4096  512 x 1 / 256 x 2: M = 1 2.55 / 2.72, M = 1000 7.05 / 7.49, M = 16384 82.8 / 83.3, M = 4096 without a residual 12.4 / 11.4
+//   K = 5120  320 x 2 / 256 x 3 / 768 x 1: M = 1 2.95 / 3.08 / 2.95, M = 4096 24.9 / 25.4 / 26.8
+//   K = 8192  512 x 2 / 1024 x 1 / 256 x 4: M = 1 3.23 / 3.40 / 3.56, M = 4096 35.5 / 36.5 / 36.1
+//   K = 11008 512 x 3 / 768 x 2: M = 1 3.78 / 3.74, M = 4096 59.3 / 59.3;  K = 16384 512 x 4 / 1024 x 2: M = 1 4.42 / 4.40, M = 4096 89.6 / 101
+//   K = 20480 512 x 6 / 1024 x 3: M = 1 5.66 / 5.29, M = 2000 54.4 / 63.7;  K = 32768 1024 x 4 / 512 x 8: M = 1 6.63 / 7.14, M = 2000 102 / 102
+//   K = 65536, walked twice by 1024 / 512: M = 1 12.5 / 13.4, M = 300 42.7 / 45.5
 template <int XDT, int FORM, bool RES>
 int launch(const NormParams& p, int64_t rows, hipStream_t st) {
   const int nchunk = p.K >> 3;
   const dim3 grid((unsigned)rows);
 #define SERQ_NORM(KT, NC) hipLaunchKernelGGL((rmsnorm_quantize_kernel<XDT, FORM, KT, NC, RES>), grid, dim3(KT), 0, st, p)
-  if (nchunk <= 128) SERQ_NORM(64, 2);
-  else if (nchunk <= 256) SERQ_NORM(128, 2);
-  else if (nchunk <= 512) SERQ_NORM(256, 2);
+  if constexpr (!RES) {
+    if (rows > 1000 && nchunk > 256 && nchunk <= 512) {
+      if (nchunk <= 384) SERQ_NORM(192, 2);
+      else SERQ_NORM(256, 2);
+      return hipGetLastError() == hipSuccess ? SERQ_OK : SERQ_EHIP;
+    }
+  }
+  if (nchunk <= 64) SERQ_NORM(64, 1);
+  else if (nchunk <= 128) SERQ_NORM(128, 1);
+  else if (nchunk <= 192) SERQ_NORM(192, 1);
+  else if (nchunk <= 256) SERQ_NORM(256, 1);
+  else if (nchunk <= 384) SERQ_NORM(384, 1);
+  else if (nchunk <= 512) SERQ_NORM(512, 1);
+  else if (nchunk <= 640) SERQ_NORM(320, 2);
+  else if (nchunk <= 768) SERQ_NORM(384, 2);
   else if (nchunk <= 1024) SERQ_NORM(512, 2);
-  else if (nchunk <= 2048) SERQ_NORM(1024, 2);
+  else if (nchunk <= 1536) SERQ_NORM(512, 3);
+  else if (nchunk <= 2048) SERQ_NORM(512, 4);
+  else if (nchunk <= 3072) SERQ_NORM(512, 6);
   else if (nchunk <= 4096) SERQ_NORM(1024, 4);
-  else SERQ_NORM(512, 0);
+  else SERQ_NORM(1024, 0);
 #undef SERQ_NORM
   return hipGetLastError() == hipSuccess ? SERQ_OK : SERQ_EHIP;
 }

@@ -76,7 +76,7 @@ def test_oracle_by_hand():
     u, rstd = orc.rmsnorm_rows(h, gain, 0.0)
     assert u[0, 0] == 6 and u[0, 1] == 8 and rstd[0] == np.float32(1.6) and rstd[1] == 0 and rstd[2] == 1
     codes, scale = orc.rmsnorm_quantize_act(h, gain, 0.0, 8)
-    assert list(codes[0, :2]) == [95, 127] and scale[0] == np.float32(np.float32(8) / np.float32(127)) * np.float32(1.6)
+    assert list(codes[0, :2]) == [95, 127] and scale[0] == np.float32(8) * (np.float32(1) / np.float32(127)) * np.float32(1.6)
     assert scale[1] == 1 and not codes[1].any()
     codes, E = orc.mx_rmsnorm_quantize_act(h, gain, 0.0)              # 9.6, 12.8: 2^3 over the largest code's 2^2 -> 2^1: 4.8, 6.4 -> 4, 6
     assert E[0, 0] == 128 and list(codes[0, :2]) == [6, 7]
