@@ -75,6 +75,20 @@ int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_heads,
                    void* q_out, int64_t ldqo, int64_t ldqoh, void* stream);
 
 /*
+ * The same for models that normalise the queries and keys of every head: before the rotation
+ *   x[d] = fl(fl(x[d] * r) * weight[d]),   r = 1 / sqrt(mean_d x[d]^2 + eps) over the head's dim channels,
+ * r formed in 64 bits, rounded to fp32, at most the largest finite number (0 where the root is 0).  q_weight for queries, k_weight for keys: [dim] fp32,
+ * 16-byte aligned, the same for all heads; NULL: those are not normalised (both NULL: serq_kv_append).  Values are never normalised.  eps finite, not
+ * negative.  Everything else as serq_kv_append.
+ */
+int serq_kv_append_norm(const void* q, int64_t ldq, int64_t ldqh, int q_heads,
+                        const void* k, int64_t ldk, int64_t ldkh, const void* v, int64_t ldv, int64_t ldvh, int dtype,
+                        const float* q_weight, const float* k_weight, float eps,
+                        const float* cos_table, const float* sin_table, int64_t table_rows, int rot_dim, int interleaved,
+                        const int32_t* positions, const serq_kv_cache* cache, const serq_kv_batch* batch,
+                        void* q_out, int64_t ldqo, int64_t ldqoh, void* stream);
+
+/*
  * Attention over the cache: query head h reads key head h / (q_heads / cache->heads),
  *   s_j = scale * q[t,h,:] . K_j,   out[t,h,:] = sum_j softmax(s)_j V_j,   lse[t,h] = log sum_j exp(s_j),
  * over the positions j with 0 <= j <= p and, where window > 0, j > p - window.  A row that sees no key (p < 0) gives out = 0,

@@ -73,6 +73,8 @@ SIGNATURES = {
     "serq_proto_gemm_i32": (_i, [_vp, _vp, _i, _i64, _i64, _i64, _vp, _i64, _vp]),
     "serq_kv_append": (_i, [_vp, _i64, _i64, _i, _vp, _i64, _i64, _vp, _i64, _i64, _i, _vp, _vp, _i64, _i, _i, _vp, _vp, _vp,
                             _vp, _i64, _i64, _vp]),
+    "serq_kv_append_norm": (_i, [_vp, _i64, _i64, _i, _vp, _i64, _i64, _vp, _i64, _i64, _i, _vp, _vp, C.c_float, _vp, _vp, _i64, _i, _i, _vp,
+                                 _vp, _vp, _vp, _i64, _i64, _vp]),
     "serq_paged_attn": (_i, [_vp, _i64, _i64, _i, _i, _vp, _vp, _i, _i64, C.c_float, _i, _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
     "serq_paged_attn_workspace_bytes": (_sz, [_i64, _i, _i, _i64, _i, _i, _i]),
     "serq_bench_mfma_peak": (_i, [_vp, _i, _i, _vp, _vp]),
@@ -90,7 +92,7 @@ _FAST = ["serq_quantize_act", "serq_swiglu_quantize_act", "serq_mx_quantize_act"
 # ... and in that of its bind_kv()
 _FAST_KV = ["serq_kv_append", "serq_paged_attn"]
 # ... and in that of its bind_norm()
-_FAST_NORM = ["serq_rmsnorm_quantize_act", "serq_rmsnorm_quantize_act_asym", "serq_mx_rmsnorm_quantize_act"]
+_FAST_NORM = ["serq_rmsnorm_quantize_act", "serq_rmsnorm_quantize_act_asym", "serq_mx_rmsnorm_quantize_act", "serq_kv_append_norm"]
 
 
 class SerqError(RuntimeError):
@@ -788,17 +790,24 @@ def _kv_structs(K, V, table, cu_q, kv_len, tokens, dtype, k_scale, v_scale):
 def kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor,
               cu_q: torch.Tensor, kv_len: torch.Tensor, cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
               interleaved: bool = False, positions: Optional[torch.Tensor] = None, k_scale: Optional[torch.Tensor] = None,
-              v_scale: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+              v_scale: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, q_norm: Optional[torch.Tensor] = None,
+              k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6) -> Optional[torch.Tensor]:
     """serq_kv_append: rotates q and k (tables cos, sin [positions, rotated channels / 2] fp32; None: no rotation), puts k and v into
-    the paged cache K, V [pages, page_size, heads, dim]; returns the rotated q (q None: keys and values only)."""
+    the paged cache K, V [pages, page_size, heads, dim]; returns the rotated q (q None: keys and values only).  With q_norm, k_norm [dim] fp32
+    (either may be None) serq_kv_append_norm: every head of q, of k is normalised by its root mean square first."""
     if q is not None and q_out is None:
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    rc = (_fast or _native()).kv_append(q, k, v, K, V, table, cu_q, kv_len, cos, sin, 1 if interleaved else 0, positions, k_scale, v_scale,
-                                        q_out)
+    normed = q_norm is not None or k_norm is not None
+    if normed:
+        rc = (_fast or _native()).kv_append_norm(q, k, v, K, V, table, cu_q, kv_len, cos, sin, 1 if interleaved else 0, positions, k_scale,
+                                                 v_scale, q_out, q_norm, k_norm, eps)
+    else:
+        rc = (_fast or _native()).kv_append(q, k, v, K, V, table, cu_q, kv_len, cos, sin, 1 if interleaved else 0, positions, k_scale, v_scale,
+                                            q_out)
     if rc == 0:
         return q_out
     if rc is not None:
-        raise SerqError("serq_kv_append", rc)
+        raise SerqError("serq_kv_append_norm" if normed else "serq_kv_append", rc)
     D = K.shape[-1]
     for t, what in ((k, "k"), (v, "v"), (q, "q"), (q_out, "q_out")):
         if t is not None:
@@ -819,12 +828,17 @@ def kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, K: to
                                   or positions.shape[0] < k.shape[0] or (positions.numel() > 1 and positions.stride(0) != 1)):
         raise ValueError("positions must be int32 [tokens] in device memory")
     c, b = _kv_structs(K, V, table, cu_q, kv_len, k.shape[0], k.dtype, k_scale, v_scale)
-    rc = lib().serq_kv_append(_ptr(q), q.stride(0) if q is not None else 0, q.stride(1) if q is not None else 0,
-                              q.shape[1] if q is not None else 0, _ptr(k), k.stride(0), k.stride(1), _ptr(v), v.stride(0), v.stride(1),
-                              _DT[k.dtype], _ptr(cos), _ptr(sin), rows, rot, 1 if interleaved else 0, _ptr(positions), C.addressof(c),
-                              C.addressof(b), _ptr(q_out), q_out.stride(0) if q is not None else 0,
-                              q_out.stride(1) if q is not None else 0, _stream())
-    _check("serq_kv_append", rc)
+    for t, what in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        if t is not None and (not t.is_cuda or t.dtype != torch.float32 or t.shape != (D,) or not t.is_contiguous()):
+            raise ValueError(f"{what} must be fp32 [dim] in device memory")
+    head = (_ptr(q), q.stride(0) if q is not None else 0, q.stride(1) if q is not None else 0, q.shape[1] if q is not None else 0,
+            _ptr(k), k.stride(0), k.stride(1), _ptr(v), v.stride(0), v.stride(1), _DT[k.dtype])
+    tail = (_ptr(cos), _ptr(sin), rows, rot, 1 if interleaved else 0, _ptr(positions), C.addressof(c), C.addressof(b), _ptr(q_out),
+            q_out.stride(0) if q is not None else 0, q_out.stride(1) if q is not None else 0, _stream())
+    if normed:
+        _check("serq_kv_append_norm", lib().serq_kv_append_norm(*head, _ptr(q_norm), _ptr(k_norm), eps, *tail))
+    else:
+        _check("serq_kv_append", lib().serq_kv_append(*head, *tail))
     return q_out
 
 

@@ -32,6 +32,7 @@ decltype(&serq_paged_attn) f_paged_attn;
 decltype(&serq_rmsnorm_quantize_act) f_rmsnorm_quantize_act;
 decltype(&serq_rmsnorm_quantize_act_asym) f_rmsnorm_quantize_act_asym;
 decltype(&serq_mx_rmsnorm_quantize_act) f_mx_rmsnorm_quantize_act;
+decltype(&serq_kv_append_norm) f_kv_append_norm;
 
 // Arguments of one call; `ok` falls once one of them is not the plain thing.
 struct Args {
@@ -360,42 +361,66 @@ PyObject* mx_rmsnorm_quantize_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 bool same_rows(const Heads& a, const Heads& b) { return a.T == b.T && a.D == b.D && a.dt == b.dt; }
 
-// q, k, v, K, V, table, cu_q, kv_len, cos, sin, interleaved, positions, k_scale, v_scale, q_out
+// q, k, v, K, V, table, cu_q, kv_len, cos, sin, interleaved, positions, k_scale, v_scale, q_out: what both appends take
+struct Append {
+  Heads q, k, v, qo;
+  Cache c;
+  const float *cs, *sn;
+  int64_t rows, rot;
+  int inter;
+  const int32_t* pos;
+};
+Append append(Args& x) {
+  Heads q{}, qo{};
+  const Heads k = heads(x, 1), v = heads(x, 2);
+  if (x.a[0] != Py_None) {
+    q = heads(x, 0);
+    qo = heads(x, 14);
+    if (!same_rows(q, k) || !same_rows(qo, k) || q.H != qo.H || q.H > 65536) x.ok = false;
+  }
+  const Cache c = cache(x, 3, 12, k);
+  const float *cs = nullptr, *sn = nullptr;
+  int64_t rows = 0, rot = 0;
+  if (x.a[8] != Py_None) {
+    const at::Tensor *ct = typed(x, 8, at::kFloat, 2), *st = typed(x, 9, at::kFloat, 2);
+    if (x.ok && (!ct->is_contiguous() || !st->is_contiguous() || ct->sizes() != st->sizes() || ct->size(1) > 65536)) x.ok = false;
+    if (x.ok) {
+      cs = (const float*)ct->data_ptr();
+      sn = (const float*)st->data_ptr();
+      rows = ct->size(0);
+      rot = 2 * ct->size(1);
+    }
+  } else if (x.a[9] != Py_None) {
+    x.ok = false;
+  }
+  const int inter = x.integer32(10);
+  const int32_t* pos = nullptr;
+  if (x.a[11] != Py_None) {
+    const at::Tensor* t = typed(x, 11, at::kInt, 1);
+    if (t && t->size(0) < k.T) x.ok = false;
+    if (t) pos = (const int32_t*)t->data_ptr();
+  }
+  if (!same_rows(k, v) || k.H != c.c.heads || v.H != c.c.heads) x.ok = false;
+  return {q, k, v, qo, c, cs, sn, rows, rot, inter, pos};
+}
 PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return run(a, n, 15, [](Args& x) {
-    Heads q{}, qo{};
-    const Heads k = heads(x, 1), v = heads(x, 2);
-    if (x.a[0] != Py_None) {
-      q = heads(x, 0);
-      qo = heads(x, 14);
-      if (!same_rows(q, k) || !same_rows(qo, k) || q.H != qo.H || q.H > 65536) x.ok = false;
-    }
-    const Cache c = cache(x, 3, 12, k);
-    const float *cs = nullptr, *sn = nullptr;
-    int64_t rows = 0, rot = 0;
-    if (x.a[8] != Py_None) {
-      const at::Tensor *ct = typed(x, 8, at::kFloat, 2), *st = typed(x, 9, at::kFloat, 2);
-      if (x.ok && (!ct->is_contiguous() || !st->is_contiguous() || ct->sizes() != st->sizes() || ct->size(1) > 65536)) x.ok = false;
-      if (x.ok) {
-        cs = (const float*)ct->data_ptr();
-        sn = (const float*)st->data_ptr();
-        rows = ct->size(0);
-        rot = 2 * ct->size(1);
-      }
-    } else if (x.a[9] != Py_None) {
-      x.ok = false;
-    }
-    const int inter = x.integer32(10);
-    const int32_t* pos = nullptr;
-    if (x.a[11] != Py_None) {
-      const at::Tensor* t = typed(x, 11, at::kInt, 1);
-      if (t && t->size(0) < k.T) x.ok = false;
-      if (t) pos = (const int32_t*)t->data_ptr();
-    }
-    if (!same_rows(k, v) || k.H != c.c.heads || v.H != c.c.heads) x.ok = false;
+    const Append r = append(x);
     return [=](void* st) {
-      return f_kv_append(q.p, q.ld, q.ldh, (int)q.H, k.p, k.ld, k.ldh, v.p, v.ld, v.ldh, k.dt, cs, sn, rows, (int)rot, inter, pos, &c.c, &c.b,
-                         qo.p, qo.ld, qo.ldh, st);
+      return f_kv_append(r.q.p, r.q.ld, r.q.ldh, (int)r.q.H, r.k.p, r.k.ld, r.k.ldh, r.v.p, r.v.ld, r.v.ldh, r.k.dt, r.cs, r.sn, r.rows, (int)r.rot,
+                         r.inter, r.pos, &r.c.c, &r.c.b, r.qo.p, r.qo.ld, r.qo.ldh, st);
+    };
+  });
+}
+
+// ..., q_norm, k_norm, eps
+PyObject* kv_append_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(a, n, 18, [](Args& x) {
+    const Append r = append(x);
+    const float *qw = scales(x, 15, r.k.D), *kw = scales(x, 16, r.k.D), eps = x.real(17);
+    return [=](void* st) {
+      return f_kv_append_norm(r.q.p, r.q.ld, r.q.ldh, (int)r.q.H, r.k.p, r.k.ld, r.k.ldh, r.v.p, r.v.ld, r.v.ldh, r.k.dt, qw, kw, eps, r.cs, r.sn,
+                              r.rows, (int)r.rot, r.inter, r.pos, &r.c.c, &r.c.b, r.qo.p, r.qo.ld, r.qo.ldh, st);
     };
   });
 }
@@ -457,7 +482,8 @@ PyObject* bind_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return bind_slots(slots, sizeof(slots) / sizeof(slots[0]), a, n);
 }
 PyObject* bind_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void** const slots[] = {(void**)&f_rmsnorm_quantize_act, (void**)&f_rmsnorm_quantize_act_asym, (void**)&f_mx_rmsnorm_quantize_act};
+  void** const slots[] = {(void**)&f_rmsnorm_quantize_act, (void**)&f_rmsnorm_quantize_act_asym, (void**)&f_mx_rmsnorm_quantize_act,
+                          (void**)&f_kv_append_norm};
   return bind_slots(slots, sizeof(slots) / sizeof(slots[0]), a, n);
 }
 
@@ -466,7 +492,7 @@ PyMethodDef methods[] = {SERQ_FAST(bind), SERQ_FAST(quantize_act), SERQ_FAST(swi
                          SERQ_FAST(mx_swiglu_quantize_act), SERQ_FAST(quantize_act_asym), SERQ_FAST(linear),
                          SERQ_FAST(mx_linear), SERQ_FAST(g128_linear), SERQ_FAST(bind_kv), SERQ_FAST(kv_append),
                          SERQ_FAST(paged_attention), SERQ_FAST(bind_norm), SERQ_FAST(rmsnorm_quantize_act),
-                         SERQ_FAST(rmsnorm_quantize_act_asym), SERQ_FAST(mx_rmsnorm_quantize_act), {nullptr, nullptr, 0, nullptr}};
+                         SERQ_FAST(rmsnorm_quantize_act_asym), SERQ_FAST(mx_rmsnorm_quantize_act), SERQ_FAST(kv_append_norm), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -4,7 +4,10 @@
 // an element.  So it is bound by bytes, and for few tokens by the latency of one chain of loads: the sequence's end -> its length and
 // number of new tokens -> the page -> the store.  A thread owns two pieces of 8 channels that the rotation mixes (the same piece of both
 // halves, or 16 neighbours), so that nothing is exchanged between threads and every access is 16 bytes wide.
+#include <type_traits>
+
 #include "kv_cache.h"
+#include "root64.h"
 
 namespace serq {
 namespace {
@@ -15,6 +18,8 @@ struct AppendParams {
   const float* cos; const float* sin; const int32_t* positions;
   int rows, rot, q_heads, items;                              // items: pairs of pieces of a token
   KvView c;
+  const float* qw; const float* kw;                           // weights of the heads' norms
+  double eps;
 };
 
 template <int DT>
@@ -42,14 +47,19 @@ __device__ __forceinline__ void turn(float& x, float& y, float c, float s) {
   y = yc + xs;
 }
 
+struct NoWeights {};
+struct HeadWeights { const float* w; v4f wx[2], wy[2]; };     // of the head's norm (or none), for the two pieces
+
 // One token a workgroup, one pair of pieces a thread (more where a token has more pairs than threads).  What does not hang on the token's place is
 // asked for before that is known: the token's values with the ends and lengths of the sequences, then the page with the rotation.
-template <int DT, bool F8, int D, bool INTER>
+// NORM: queries and keys of every head are normalised before they are turned.  The D / 16 threads that have a head's pieces are neighbours, so its sum of
+// squares takes two or three exchanges between lanes; the weights are asked for with the values.
+template <int DT, bool F8, int D, bool INTER, bool NORM>
 __global__ __launch_bounds__(512) void kv_append_kernel(AppendParams p) {
   constexpr int PP = D / 16;                                  // pairs of a head
   const int t = blockIdx.x, lane = threadIdx.x & 63;
 
-  struct Item {
+  struct Item : std::conditional_t<NORM, HeadWeights, NoWeights> {
     int h, d0, d1;                                            // head of its kind, first channels of the two pieces
     bool is_q, is_k, rotated;
     Raw8<DT> x, y;
@@ -67,6 +77,16 @@ __global__ __launch_bounds__(512) void kv_append_kernel(AppendParams p) {
     const char* src = m.is_q ? p.q + t * p.ldq + m.h * p.ldqh : m.is_k ? p.k + t * p.ldk + m.h * p.ldkh : p.v + t * p.ldv + m.h * p.ldvh;
     m.x.a = *(const u4*)(src + 2 * m.d0);
     m.y.a = *(const u4*)(src + 2 * m.d1);
+    if constexpr (NORM) {
+      m.w = m.is_q ? p.qw : m.is_k ? p.kw : nullptr;
+      if (m.w) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          m.wx[i] = *(const v4f*)(m.w + m.d0 + 4 * i);
+          m.wy[i] = *(const v4f*)(m.w + m.d1 + 4 * i);
+        }
+      }
+    }
     return m;
   };
   // (the sequences first: loads come back in their order)
@@ -106,6 +126,24 @@ __global__ __launch_bounds__(512) void kv_append_kernel(AppendParams p) {
     float a[8], e[8];
     values8<DT>(m.x, a);
     values8<DT>(m.y, e);
+    if constexpr (NORM) {
+      if (m.w) {                                              // (for all threads of a head or none)
+        double s = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = __builtin_fma((double)a[i], (double)a[i], s);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = __builtin_fma((double)e[i], (double)e[i], s);
+        s = dpp_add<kDpp1>(s);
+        s = dpp_add<kDpp2>(s);
+        if constexpr (PP == 8) s = dpp_add<kDppMirror8>(s);
+        const float r = inv_root(__builtin_fma(s, 1.0 / D, p.eps));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          a[i] = a[i] * r * m.wx[i / 4][i % 4];
+          e[i] = e[i] * r * m.wy[i / 4][i % 4];
+        }
+      }
+    }
     if (m.rotated) {
       const int64_t at = (int64_t)turned * (p.rot / 2) + (INTER ? m.d0 / 2 : m.d0);
       float c[8], s[8];
@@ -147,11 +185,15 @@ __global__ __launch_bounds__(512) void kv_append_kernel(AppendParams p) {
   }
 }
 
+template <int DT, bool F8, int D, bool INTER>
+void launch_inter(const AppendParams& p, hipStream_t st) {
+  const dim3 threads(p.items >= 512 ? 512 : (p.items + 63) & ~63);
+  if (p.qw || p.kw) hipLaunchKernelGGL((kv_append_kernel<DT, F8, D, INTER, true>), dim3(p.c.tokens), threads, 0, st, p);
+  else hipLaunchKernelGGL((kv_append_kernel<DT, F8, D, INTER, false>), dim3(p.c.tokens), threads, 0, st, p);
+}
 template <int DT, bool F8, int D>
 void launch(const AppendParams& p, bool inter, hipStream_t st) {
-  const int threads = p.items >= 512 ? 512 : (p.items + 63) & ~63;
-  if (inter) hipLaunchKernelGGL((kv_append_kernel<DT, F8, D, true>), dim3(p.c.tokens), dim3(threads), 0, st, p);
-  else hipLaunchKernelGGL((kv_append_kernel<DT, F8, D, false>), dim3(p.c.tokens), dim3(threads), 0, st, p);
+  inter ? launch_inter<DT, F8, D, true>(p, st) : launch_inter<DT, F8, D, false>(p, st);
 }
 
 }  // namespace
@@ -159,9 +201,10 @@ void launch(const AppendParams& p, bool inter, hipStream_t st) {
 
 using namespace serq;
 
-extern "C" int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_heads,
+extern "C" int serq_kv_append_norm(const void* q, int64_t ldq, int64_t ldqh, int q_heads,
                               const void* k, int64_t ldk, int64_t ldkh, const void* v, int64_t ldv, int64_t ldvh, int dtype,
-                              const float* cos_table, const float* sin_table, int64_t table_rows, int rot_dim, int interleaved,
+                              const float* q_weight, const float* k_weight, float eps, const float* cos_table, const float* sin_table, int64_t table_rows,
+                              int rot_dim, int interleaved,
                               const int32_t* positions, const serq_kv_cache* cache, const serq_kv_batch* batch,
                               void* q_out, int64_t ldqo, int64_t ldqoh, void* stream) {
   AppendParams p{};
@@ -171,6 +214,7 @@ extern "C" int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_he
   if (q_heads < 0 || q_heads > 65536) return SERQ_ESHAPE;
   if (rot_dim < 0 || rot_dim > D || (rot_dim % 16) != 0 || table_rows < 0 || table_rows > 0x7fffffff) return SERQ_ESHAPE;
   if (rot_dim > 0 && table_rows == 0) return SERQ_ESHAPE;
+  if (!(eps >= 0.0f) || !(eps <= FLT_MAX)) return SERQ_ESHAPE;
   if (batch->tokens == 0 || batch->seqs == 0) return SERQ_OK;
   if (q_heads > 0) {
     if ((rc = kv_check_rows(q, ldq, ldqh, q_heads, D)) != SERQ_OK) return rc;
@@ -183,11 +227,12 @@ extern "C" int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_he
     if (!cos_table || !sin_table) return SERQ_ENULL;
     if (!kv_aligned(cos_table, 16) || !kv_aligned(sin_table, 16)) return SERQ_EALIGN;
   }
-  if (!kv_aligned(positions, 4)) return SERQ_EALIGN;
+  if (!kv_aligned(positions, 4) || !kv_aligned(q_weight, 16) || !kv_aligned(k_weight, 16)) return SERQ_EALIGN;
   p.q = (const char*)q; p.k = (const char*)k; p.v = (const char*)v; p.qo = (char*)q_out;
   p.ldq = 2 * ldq; p.ldqh = 2 * ldqh; p.ldk = 2 * ldk; p.ldkh = 2 * ldkh; p.ldv = 2 * ldv; p.ldvh = 2 * ldvh;
   p.ldqo = 2 * ldqo; p.ldqoh = 2 * ldqoh;
   p.cos = cos_table; p.sin = sin_table; p.positions = positions;
+  p.qw = q_heads > 0 ? q_weight : nullptr; p.kw = k_weight; p.eps = (double)eps;
   p.rows = (int)table_rows; p.rot = rot_dim; p.q_heads = q_heads;
   p.items = (q_heads + 2 * cache->heads) * (D / 16);
   const bool f8 = cache->dtype == SERQ_F8, bf = dtype == SERQ_BF16, inter = interleaved != 0;
@@ -200,4 +245,13 @@ extern "C" int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_he
     else f8 ? launch<SERQ_F16, true, 64>(p, inter, st) : launch<SERQ_F16, false, 64>(p, inter, st);
   }
   return hipGetLastError() == hipSuccess ? SERQ_OK : SERQ_EHIP;
+}
+
+extern "C" int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_heads,
+                              const void* k, int64_t ldk, int64_t ldkh, const void* v, int64_t ldv, int64_t ldvh, int dtype,
+                              const float* cos_table, const float* sin_table, int64_t table_rows, int rot_dim, int interleaved,
+                              const int32_t* positions, const serq_kv_cache* cache, const serq_kv_batch* batch,
+                              void* q_out, int64_t ldqo, int64_t ldqoh, void* stream) {
+  return serq_kv_append_norm(q, ldq, ldqh, q_heads, k, ldk, ldkh, v, ldv, ldvh, dtype, nullptr, nullptr, 0.0f, cos_table, sin_table, table_rows, rot_dim,
+                             interleaved, positions, cache, batch, q_out, ldqo, ldqoh, stream);
 }
