@@ -118,6 +118,35 @@ int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int d
                     void* workspace, size_t workspace_bytes, void* stream);
 size_t serq_paged_attn_workspace_bytes(int64_t tokens, int seqs, int max_q, int64_t max_kv, int q_heads, int kv_heads, int dim);
 
+/*
+ * The same with what some models put between the scores and the softmax.  A row of token t at position p has the scores
+ *   s_j = scale * q.K_j                             (plain)
+ *   s_j = cap * tanh(scale * q.K_j / cap)           (cap > 0)
+ *   s_j = scale * q.K_j - slopes[h] * |p - j|       (slopes)
+ * over the keys j with see_from[t] <= j < see_to[t] that lie in the sequence (0 <= j < L_b) and, where window > 0, j > p - window.  Without see_from
+ * rows see from 0, without see_to up to their own position (p + 1): several documents one after the other in a sequence have the start of each row's
+ * own in see_from; a prefix that all its rows see, both ways, has its length in see_to of those rows; a row of padding has 0 there.  A row that
+ * sees no key gives out = 0, lse = -inf; lse is of the scores as above.
+ *   mod NULL, or all of it zero: serq_paged_attn.  cap and slopes together: SERQ_EUNSUPPORTED.
+ * What a row does not see does not reach its result, as above.  Pages between the first and the last key that a sequence's rows see may be read whatever lies between
+ * (their page numbers are clamped); pages outside are not.  With a cap a product of -inf has the score -cap and weighs as such.  A capped score is good to
+ * cap * 2^-20 beside what scale * q.K_j is; a biased one is an fp32 sum that the bias is part of, so it is good to about
+ * 2^-24 (dim + 8) slopes[h] |p - j| (of no account where a row sees keys near its own; a row whose nearest key has a bias beyond 2^24 may count as one that sees none).
+ * Everything else (workspace, bounds, types) as serq_paged_attn.
+ */
+#define SERQ_ATTN_MAX_CAP 1024.0f
+typedef struct serq_attn_mod {
+  const float*   slopes;          /* [q_heads] fp32, finite, or NULL */
+  const int32_t* see_from;        /* [tokens], or NULL */
+  const int32_t* see_to;          /* [tokens], or NULL */
+  float          cap;             /* up to SERQ_ATTN_MAX_CAP; 0: none */
+} serq_attn_mod;
+
+int serq_paged_attn_mod(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int dtype, const serq_kv_cache* cache,
+                        const serq_kv_batch* batch, int max_q, int64_t max_kv, float scale, int window, const serq_attn_mod* mod,
+                        void* out, int64_t ldo, int64_t ldoh, float* lse,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

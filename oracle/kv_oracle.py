@@ -71,3 +71,42 @@ def attention(q, K, V, scale, first, window=0):
         mag[i] = (e @ np.abs(v) / total).reshape(Hq, D)
         big[i] = scale * (np.abs(x) @ np.abs(k)).max(-1).reshape(Hq)
     return out, lse, mag, big
+
+
+def attention_mod(q, K, V, scale, first, lo, hi, cap=0.0, slopes=None, rnd=2.0 ** -24):
+    """One sequence: row i, at position first + i, sees the keys lo[i] <= j < hi[i]; scores cap tanh(s / cap), or s - slopes[h] |p - j|.  Returns
+    out, lse, sum_j softmax_j |v_j| and two error bounds of what fp32 scores do: to out (sum_j p_j e_j |v_j| + sum_j p_j e_j sum_j p_j |v_j|)
+    and to lse (sum_j p_j e_j), where e_j is the error of score j: (D + 8) rnd (scale sum_d |q_d k_d| + the bias), 3 rnd of the bias for its own products,
+    and 12 rnd cap for a capped score (the reciprocal, the exponential, their arguments and the sum: 2.75 2^-22 cap)."""
+    n, Hq, D = q.shape
+    H = K.shape[1]
+    G = Hq // H
+    out, mag, eo = np.zeros((n, Hq, D)), np.zeros((n, Hq, D)), np.zeros((n, Hq, D))
+    lse, el = np.full((n, Hq), -np.inf), np.zeros((n, Hq))
+    sl = None if slopes is None else np.asarray(slopes, np.float64).reshape(H, G, 1)
+    for i in range(n):
+        a, b = int(lo[i]), int(hi[i])
+        if b <= a:
+            continue
+        x = q[i].reshape(H, G, D)
+        k, v = K[a:b].transpose(1, 2, 0), V[a:b].transpose(1, 0, 2)              # [H, D, keys], [H, keys, D]
+        s = scale * (x @ k)                                                      # [H, G, keys]
+        e = (D + 8) * rnd * scale * (np.abs(x) @ np.abs(k))
+        if cap:
+            s = cap * np.tanh(s / cap)
+            e = e + 12 * rnd * cap
+        if sl is not None:
+            far = sl * np.abs(first + i - np.arange(a, b))
+            s = s - far
+            e = e + (D + 11) * rnd * np.abs(far)
+        m = s.max(-1, keepdims=True)
+        p = np.exp(s - m)
+        total = p.sum(-1, keepdims=True)
+        lse[i] = (m + np.log(total)).reshape(Hq)
+        p = p / total
+        off = (p * e).sum(-1, keepdims=True)
+        out[i] = (p @ v).reshape(Hq, D)
+        mag[i] = (p @ np.abs(v)).reshape(Hq, D)
+        eo[i] = ((p * e) @ np.abs(v) + off * (p @ np.abs(v))).reshape(Hq, D)
+        el[i] = off.reshape(Hq)
+    return out, lse, mag, eo, el

@@ -76,6 +76,7 @@ SIGNATURES = {
     "serq_kv_append_norm": (_i, [_vp, _i64, _i64, _i, _vp, _i64, _i64, _vp, _i64, _i64, _i, _vp, _vp, C.c_float, _vp, _vp, _i64, _i, _i, _vp,
                                  _vp, _vp, _vp, _i64, _i64, _vp]),
     "serq_paged_attn": (_i, [_vp, _i64, _i64, _i, _i, _vp, _vp, _i, _i64, C.c_float, _i, _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
+    "serq_paged_attn_mod": (_i, [_vp, _i64, _i64, _i, _i, _vp, _vp, _i, _i64, C.c_float, _i, _vp, _vp, _i64, _i64, _vp, _vp, _sz, _vp]),
     "serq_paged_attn_workspace_bytes": (_sz, [_i64, _i, _i, _i64, _i, _i, _i]),
     "serq_bench_mfma_peak": (_i, [_vp, _i, _i, _vp, _vp]),
     "serq_bench_mfma_fp4_peak": (_i, [_vp, _i, _i, _vp, _vp]),
@@ -92,7 +93,8 @@ _FAST = ["serq_quantize_act", "serq_swiglu_quantize_act", "serq_mx_quantize_act"
 # ... and in that of its bind_kv()
 _FAST_KV = ["serq_kv_append", "serq_paged_attn"]
 # ... and in that of its bind_norm()
-_FAST_NORM = ["serq_rmsnorm_quantize_act", "serq_rmsnorm_quantize_act_asym", "serq_mx_rmsnorm_quantize_act", "serq_kv_append_norm"]
+_FAST_NORM = ["serq_rmsnorm_quantize_act", "serq_rmsnorm_quantize_act_asym", "serq_mx_rmsnorm_quantize_act", "serq_kv_append_norm",
+              "serq_paged_attn_mod"]
 
 
 class SerqError(RuntimeError):
@@ -753,6 +755,11 @@ class _KvBatch(C.Structure):
                 ("table_width", C.c_int32), ("seqs", C.c_int32)]
 
 
+class _AttnMod(C.Structure):
+    """serq_attn_mod (include/serq_kv.h)."""
+    _fields_ = [("slopes", _vp), ("see_from", _vp), ("see_to", _vp), ("cap", C.c_float)]
+
+
 def _heads(T: torch.Tensor, what: str, dim: Optional[int] = None):
     if not T.is_cuda:
         raise ValueError(f"{what} must live in device memory")
@@ -856,18 +863,26 @@ def paged_attention_workspace(tokens: int, seqs: int, max_q: int, max_kv: int, q
 def paged_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor,
                     max_q: int, max_kv: int, scale: Optional[float] = None, window: int = 0, k_scale: Optional[torch.Tensor] = None,
                     v_scale: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
-                    ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+                    ws: Optional[torch.Tensor] = None, cap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                    see_from: Optional[torch.Tensor] = None, see_to: Optional[torch.Tensor] = None) -> torch.Tensor:
     """serq_paged_attn: softmax(scale q K^T) V over the cached positions up to each new token's own (scale: 1 / sqrt(dim) by default;
-    window > 0: the last `window` of them); lse [tokens, q_heads] fp32 takes the logarithm of the softmax' sum."""
+    window > 0: the last `window` of them); lse [tokens, q_heads] fp32 takes the logarithm of the softmax' sum.  serq_paged_attn_mod where one of these
+    is given: cap > 0: scores become cap tanh(score / cap); slopes [q_heads] fp32: a head's slope times the distance is taken off; see_from, see_to
+    [tokens] int32: token t sees the positions see_from[t] .. see_to[t]-1 (packed documents, prefixes seen both ways, padding)."""
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if scale is None:
         scale = q.shape[-1] ** -0.5
-    rc = (_fast or _native()).paged_attention(q, K, V, table, cu_q, kv_len, max_q, max_kv, scale, window, k_scale, v_scale, out, lse, ws)
+    modified = cap != 0 or slopes is not None or see_from is not None or see_to is not None
+    if modified:
+        rc = (_fast or _native()).paged_attention_mod(q, K, V, table, cu_q, kv_len, max_q, max_kv, scale, window, k_scale, v_scale, out, lse, ws,
+                                                      cap, slopes, see_from, see_to)
+    else:
+        rc = (_fast or _native()).paged_attention(q, K, V, table, cu_q, kv_len, max_q, max_kv, scale, window, k_scale, v_scale, out, lse, ws)
     if rc == 0:
         return out
     if rc is not None:
-        raise SerqError("serq_paged_attn", rc)
+        raise SerqError("serq_paged_attn_mod" if modified else "serq_paged_attn", rc)
     D = K.shape[-1]
     for t, what in ((q, "q"), (out, "out")):
         _heads(t, what, D)
@@ -877,9 +892,16 @@ def paged_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table: to
         raise ValueError("lse must be fp32 [tokens, q_heads] in device memory")
     if ws is not None and (not ws.is_cuda or ws.dtype != torch.uint8 or not ws.is_contiguous()):
         raise ValueError("ws must be a uint8 buffer in device memory")
+    for t, what, dt, n in ((slopes, "slopes", torch.float32, q.shape[1]), (see_from, "see_from", torch.int32, q.shape[0]),
+                           (see_to, "see_to", torch.int32, q.shape[0])):
+        if t is not None and (not t.is_cuda or t.dtype != dt or t.shape != (n,) or not t.is_contiguous()):
+            raise ValueError(f"{what} must be {'fp32 [q_heads]' if what == 'slopes' else 'int32 [tokens]'} in device memory")
     c, b = _kv_structs(K, V, table, cu_q, kv_len, q.shape[0], q.dtype, k_scale, v_scale)
-    rc = lib().serq_paged_attn(_ptr(q), q.stride(0), q.stride(1), q.shape[1], _DT[q.dtype], C.addressof(c), C.addressof(b), max_q, max_kv,
-                               scale, window, _ptr(out), out.stride(0), out.stride(1), _ptr(lse), _ptr(ws),
-                               0 if ws is None else ws.numel(), _stream())
-    _check("serq_paged_attn", rc)
+    head = (_ptr(q), q.stride(0), q.stride(1), q.shape[1], _DT[q.dtype], C.addressof(c), C.addressof(b), max_q, max_kv, scale, window)
+    tail = (_ptr(out), out.stride(0), out.stride(1), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(), _stream())
+    if modified:
+        m = _AttnMod(_ptr(slopes), _ptr(see_from), _ptr(see_to), cap)
+        _check("serq_paged_attn_mod", lib().serq_paged_attn_mod(*head, C.addressof(m), *tail))
+    else:
+        _check("serq_paged_attn", lib().serq_paged_attn(*head, *tail))
     return out

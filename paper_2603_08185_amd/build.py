@@ -13,7 +13,8 @@ LIB = os.path.join(HERE, "libserq.so")
 FASTCALL = os.path.join(HERE, "_fastcall.so")
 SOURCES = ["api.hip", "quantize_act.hip", "pack.hip", "skinny.hip", "gemm_mfma.hip", "gemm_mid.hip", "gemm_mx.hip", "gemm_mid_mx.hip", "skinny_mx.hip",
            "mx.hip", "rmsnorm.hip", "peaks.hip", "noalloc.hip", "grouped.hip", "grouped_mid.hip", "fp6.hip", "kv_append.hip",
-           "paged_attn.hip", "paged_attn_few.hip", "paged_attn_tile.hip", "paged_attn_mixed.hip"]
+           "paged_attn.hip", "paged_attn_few.hip", "paged_attn_tile.hip", "paged_attn_mixed.hip",
+           "paged_attn_ranges.hip", "paged_attn_capped.hip", "paged_attn_biased.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

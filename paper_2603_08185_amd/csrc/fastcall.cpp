@@ -33,6 +33,7 @@ decltype(&serq_rmsnorm_quantize_act) f_rmsnorm_quantize_act;
 decltype(&serq_rmsnorm_quantize_act_asym) f_rmsnorm_quantize_act_asym;
 decltype(&serq_mx_rmsnorm_quantize_act) f_mx_rmsnorm_quantize_act;
 decltype(&serq_kv_append_norm) f_kv_append_norm;
+decltype(&serq_paged_attn_mod) f_paged_attn_mod;
 
 // Arguments of one call; `ok` falls once one of them is not the plain thing.
 struct Args {
@@ -425,31 +426,64 @@ PyObject* kv_append_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// q, K, V, table, cu_q, kv_len, max_q, max_kv, scale, window, k_scale, v_scale, out, lse, ws
+// q, K, V, table, cu_q, kv_len, max_q, max_kv, scale, window, k_scale, v_scale, out, lse, ws: what both attentions take
+struct Attention {
+  Heads q, o;
+  Cache c;
+  int max_q, window;
+  int64_t max_kv;
+  float scale;
+  float* lse;
+  Room w;
+};
+Attention attention(Args& x) {
+  const Heads q = heads(x, 0), o = heads(x, 12);
+  const Cache c = cache(x, 1, 10, q);
+  const int max_q = x.integer32(6), window = x.integer32(9);
+  const int64_t max_kv = x.integer(7);
+  const float scale = x.real(8);
+  float* lse = nullptr;
+  if (x.a[13] != Py_None) {
+    const at::Tensor* t = typed(x, 13, at::kFloat, 2);
+    if (t && (!t->is_contiguous() || t->size(0) != q.T || t->size(1) != q.H)) x.ok = false;
+    if (t) lse = (float*)t->data_ptr();
+  }
+  Room w{};
+  if (x.a[14] != Py_None) {
+    const at::Tensor* t = x.ok ? x.tensor(14) : nullptr;
+    if (t && (!t->is_cuda() || t->scalar_type() != at::kByte || !t->is_contiguous())) x.ok = false;
+    if (t && x.ok) w = {t->data_ptr(), (size_t)t->numel()};
+  }
+  if (!same_rows(q, o) || q.H != o.H || q.H > 65536) x.ok = false;
+  return {q, o, c, max_q, window, max_kv, scale, lse, w};
+}
 PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return run(a, n, 15, [](Args& x) {
-    const Heads q = heads(x, 0), o = heads(x, 12);
-    const Cache c = cache(x, 1, 10, q);
-    const int max_q = x.integer32(6), window = x.integer32(9);
-    const int64_t max_kv = x.integer(7);
-    float scale = 0.0f;
-    if (PyFloat_CheckExact(x.a[8])) scale = (float)PyFloat_AS_DOUBLE(x.a[8]);
-    else x.ok = false;
-    float* lse = nullptr;
-    if (x.a[13] != Py_None) {
-      const at::Tensor* t = typed(x, 13, at::kFloat, 2);
-      if (t && (!t->is_contiguous() || t->size(0) != q.T || t->size(1) != q.H)) x.ok = false;
-      if (t) lse = (float*)t->data_ptr();
-    }
-    Room w{};
-    if (x.a[14] != Py_None) {
-      const at::Tensor* t = x.ok ? x.tensor(14) : nullptr;
-      if (t && (!t->is_cuda() || t->scalar_type() != at::kByte || !t->is_contiguous())) x.ok = false;
-      if (t && x.ok) w = {t->data_ptr(), (size_t)t->numel()};
-    }
-    if (!same_rows(q, o) || q.H != o.H || q.H > 65536) x.ok = false;
+    const Attention r = attention(x);
     return [=](void* st) {
-      return f_paged_attn(q.p, q.ld, q.ldh, (int)q.H, q.dt, &c.c, &c.b, max_q, max_kv, scale, window, o.p, o.ld, o.ldh, lse, w.p, w.n, st);
+      return f_paged_attn(r.q.p, r.q.ld, r.q.ldh, (int)r.q.H, r.q.dt, &r.c.c, &r.c.b, r.max_q, r.max_kv, r.scale, r.window, r.o.p, r.o.ld, r.o.ldh,
+                          r.lse, r.w.p, r.w.n, st);
+    };
+  });
+}
+
+// ..., cap, slopes, see_from, see_to
+PyObject* paged_attention_mod(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return run(a, n, 19, [](Args& x) {
+    const Attention r = attention(x);
+    serq_attn_mod m{};
+    m.cap = x.real(15);
+    m.slopes = scales(x, 16, r.q.H);
+    const int32_t** const see[2] = {&m.see_from, &m.see_to};
+    for (int i = 0; i < 2; ++i) {
+      if (x.a[17 + i] == Py_None) continue;
+      const at::Tensor* t = typed(x, 17 + i, at::kInt, 1);
+      if (t && t->size(0) != r.q.T) x.ok = false;
+      if (t) *see[i] = (const int32_t*)t->data_ptr();
+    }
+    return [=](void* st) {
+      return f_paged_attn_mod(r.q.p, r.q.ld, r.q.ldh, (int)r.q.H, r.q.dt, &r.c.c, &r.c.b, r.max_q, r.max_kv, r.scale, r.window, &m, r.o.p, r.o.ld,
+                              r.o.ldh, r.lse, r.w.p, r.w.n, st);
     };
   });
 }
@@ -483,7 +517,7 @@ PyObject* bind_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 PyObject* bind_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void** const slots[] = {(void**)&f_rmsnorm_quantize_act, (void**)&f_rmsnorm_quantize_act_asym, (void**)&f_mx_rmsnorm_quantize_act,
-                          (void**)&f_kv_append_norm};
+                          (void**)&f_kv_append_norm, (void**)&f_paged_attn_mod};
   return bind_slots(slots, sizeof(slots) / sizeof(slots[0]), a, n);
 }
 
@@ -492,7 +526,8 @@ PyMethodDef methods[] = {SERQ_FAST(bind), SERQ_FAST(quantize_act), SERQ_FAST(swi
                          SERQ_FAST(mx_swiglu_quantize_act), SERQ_FAST(quantize_act_asym), SERQ_FAST(linear),
                          SERQ_FAST(mx_linear), SERQ_FAST(g128_linear), SERQ_FAST(bind_kv), SERQ_FAST(kv_append),
                          SERQ_FAST(paged_attention), SERQ_FAST(bind_norm), SERQ_FAST(rmsnorm_quantize_act),
-                         SERQ_FAST(rmsnorm_quantize_act_asym), SERQ_FAST(mx_rmsnorm_quantize_act), SERQ_FAST(kv_append_norm), {nullptr, nullptr, 0, nullptr}};
+                         SERQ_FAST(rmsnorm_quantize_act_asym), SERQ_FAST(mx_rmsnorm_quantize_act), SERQ_FAST(kv_append_norm),
+                         SERQ_FAST(paged_attention_mod), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -6,6 +6,8 @@
 
 #include <float.h>
 
+#include <type_traits>
+
 #include "kv_cache.h"
 
 namespace serq {
@@ -21,6 +23,17 @@ struct AttnParams {
   float* part;            // the slots where slices meet: [row blocks][key heads][slices]; few: [workgroups][2]
   KvView c;
 };
+
+// What may stand between the scores and the softmax: rows that see a range of keys of their own; scores capped by a tanh; scores less a slope times the
+// distance (both with such ranges too, or without).
+enum Mod { kPlain, kRanges, kCapped, kBiased };
+struct AttnModParams : AttnParams {
+  const int32_t* from;    // by row of q: the first key that it sees, and the one past its last; or null
+  const int32_t* to;
+  const float* slopes;    // kBiased: by query head
+  float cap;              // kCapped
+};
+template <int MOD> using ParamsOf = std::conditional_t<MOD == kPlain, AttnParams, AttnModParams>;
 
 struct RowBlock {
   int b, tok0, r0, n, L;  // sequence, its first row of q, the block's first row, new tokens, keys
@@ -47,6 +60,68 @@ __device__ __forceinline__ RowBlock row_block(const AttnParams& p, int b, int c0
   k.all_to = min(first + 1, k.end);
   return k;
 }
+// The keys that the row of q at position pos of a sequence of L keys sees: lo <= j < hi (both 0: none).
+struct Range { int lo, hi; };
+__device__ __forceinline__ Range row_range(const AttnModParams& p, int row, int pos, int L) {
+  Range x;
+  x.hi = min(p.to ? p.to[row] : pos + 1, min(L, p.c.width << p.c.page_shift));
+  x.lo = max(p.from ? p.from[row] : 0, 0);
+  if (p.window > 0) x.lo = max(x.lo, pos - p.window + 1);
+  return x.hi > x.lo ? x : Range{0, 0};
+}
+// What rows see together: [begin, end) holds all of it, [all_from, all_to) is seen by each (empty where a row sees nothing).
+struct Seen {
+  int begin = 0x7fffffff, end = 0, all_from = 0, all_to = 0x7fffffff;
+  __device__ __forceinline__ void add(const Range& x) {
+    if (x.hi > 0) begin = min(begin, x.lo);
+    end = max(end, x.hi);
+    all_from = max(all_from, x.lo);
+    all_to = min(all_to, x.hi);
+  }
+};
+// op over the 64 lanes of a wave, the result in all of them (as wave_reduce, for whole numbers)
+template <class Op>
+__device__ __forceinline__ int wave_reduce_int(int v, const Op& op) {
+  v = op(v, __builtin_amdgcn_update_dpp(v, v, kDpp1, 0xf, 0xf, false));
+  v = op(v, __builtin_amdgcn_update_dpp(v, v, kDpp2, 0xf, 0xf, false));
+  v = op(v, __builtin_amdgcn_update_dpp(v, v, kDppMirror8, 0xf, 0xf, false));
+  v = op(v, __builtin_amdgcn_update_dpp(v, v, kDppMirror16, 0xf, 0xf, false));
+  const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+  v = op((int)a[0], (int)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+  return op((int)b[0], (int)b[1]);
+}
+__device__ __forceinline__ int wave_min_int(int v) {
+  return uniform(wave_reduce_int(v, [](int a, int b) { return min(a, b); }));
+}
+__device__ __forceinline__ int wave_max_int(int v) {
+  return uniform(wave_reduce_int(v, [](int a, int b) { return max(a, b); }));
+}
+// row_block by what each of its tokens sees; by a whole wave, whose lanes look at a token each.  (One name for both, by the parameters' type.)
+template <int BM>
+__device__ __forceinline__ RowBlock block_of(const AttnParams& p, int b, int c0, int n, int L, int r0) {
+  return row_block<BM>(p, b, c0, n, L, r0);
+}
+template <int BM>
+__device__ __forceinline__ RowBlock block_of(const AttnModParams& p, int b, int c0, int n, int L, int r0) {
+  RowBlock k;
+  const int G = p.group, lane = threadIdx.x & 63;
+  k.b = b;
+  k.tok0 = c0;
+  k.n = n;
+  k.L = L;
+  k.r0 = r0;
+  k.rows = min(n * G - r0, BM);
+  const int last = k.rows > 0 ? (r0 + k.rows - 1) / G : -1;
+  Seen s;
+  for (int i = r0 / G + lane; i <= last; i += 64) s.add(row_range(p, c0 + i, L - n + i, L));
+  k.end = wave_max_int(s.end);
+  k.begin = k.end > 0 ? wave_min_int(s.begin) : 0;
+  k.all_from = wave_max_int(s.all_from);
+  k.all_to = min(wave_min_int(s.all_to), k.end);
+  return k;
+}
+
 // whether a sequence is this kernel's (and one that can be)
 __device__ __forceinline__ bool takes(const AttnParams& p, int c0, int n) {
   return n > 0 && c0 >= 0 && n <= p.c.tokens - c0 && n * p.group >= p.rows_from && n * p.group < p.rows_to;
@@ -198,6 +273,39 @@ __device__ __forceinline__ float row_lse(float m, float l) {
   return l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.693147180559945309f;
 }
 
+// ---- scores before the softmax --------------------------------------------------------------------------------------------------
+// Biased: a slope times the distance is a number of score units that is there before the first product: the sums of the matrix instruction begin with it.
+// `slope` in units of a score (score_slope), `d` the row's position less the key's.
+__device__ __forceinline__ float score_slope(float slope, float c) { return fminf(fmaxf(slope * kLog2e / c, -FLT_MAX), FLT_MAX); }
+__device__ __forceinline__ float distance_bias(float slope, float d) { return -slope * fabsf(d); }
+
+// The reference of such scores lies higher by 2^-22 of its size where that is large: a product s c that is as large as a bias can be is rounded in m and not in s c - m, and what is
+// left may not make a weight infinite in keys so far off that they weigh nothing in the end.
+template <int MOD, int DT>
+__device__ __forceinline__ float reference_of(float score, float c) {
+  const float m = reference<DT>(score, c);
+  if constexpr (MOD == kBiased) return fabsf(m) > 4096.0f ? fminf(__builtin_fmaf(fabsf(m), 0x1p-22f, m), FLT_MAX) : m;
+  else return m;
+}
+
+// Capped: cap tanh(x) = cap - 2 cap / (1 + e^(2 x)), x = score / cap.  What stands in a score's place from here on is -1 / (1 + e^(2 x)), which grows with the
+// score, with 2 cap log2 e in the place of the scale's factor; the cap itself is the same for all keys of a row, so the softmax does not need it and the
+// logarithm of its sum gets it at the end.  Good to some 2^-23 of 2 cap log2 e in the exponent: 2^-14 of a weight for a cap of 128.
+struct Cap {
+  float rate;             // 2 log2 e / cap of what a raw score stands for
+  __device__ __forceinline__ Cap(const AttnModParams& p, float k_scale)
+      : rate(fminf(fmaxf(2.0f * kLog2e * p.scale * k_scale / p.cap, FLT_MIN), FLT_MAX)) {}
+  __device__ __forceinline__ float operator()(float s) const { return -__builtin_amdgcn_rcpf(1.0f + exp2_fast(s * rate)); }
+};
+__device__ __forceinline__ float cap_factor(float cap) { return fmaxf(2.0f * cap * kLog2e, FLT_MIN); }
+template <int MOD>
+__device__ __forceinline__ float factor_of(const ParamsOf<MOD>& p, float k_scale) {
+  if constexpr (MOD == kCapped) return cap_factor(p.cap);
+  else return score_factor(p.scale, k_scale);
+}
+__device__ __forceinline__ float lse_of(const AttnParams&, float m, float l) { return row_lse(m, l); }
+__device__ __forceinline__ float lse_of(const AttnModParams& p, float m, float l) { return l == 0.0f ? -INFINITY : row_lse(m, l) + p.cap; }   // (cap 0: none)
+
 constexpr int kMaxSlices = 256;          // of the kernel for few rows
 constexpr int kMaxTileSlices = 32;       // of the kernel for many
 constexpr int kTileRows = 128;
@@ -232,5 +340,13 @@ int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb
 size_t paged_attn_tile_slot_floats(int D);
 int launch_paged_attn_tile(const AttnParams& p, int dtype, bool f8, int D, int blocks, hipStream_t st);
 int launch_paged_attn_mixed(const AttnParams& many, const AttnParams& few, int dtype, bool f8, int D, int blocks, int shares, hipStream_t st);
+// the same three with what stands between scores and softmax; one or two of them: a call's whole launch
+struct ModLaunch {
+  const AttnModParams* many; const AttnModParams* few;        // null: none
+  int dtype; bool f8; int D, nb, blocks, shares;              // blocks: of the kernel for many rows, shares: workgroups of the one for few
+};
+int launch_paged_attn_ranges(const ModLaunch& a, hipStream_t st);
+int launch_paged_attn_capped(const ModLaunch& a, hipStream_t st);
+int launch_paged_attn_biased(const ModLaunch& a, hipStream_t st);
 
 }  // namespace serq

@@ -157,30 +157,39 @@ size_t serq_paged_attn_workspace_bytes(int64_t tokens, int seqs, int max_q, int6
   return most_bytes(tokens, seqs, max_q, max_kv, kv_heads, q_heads / kv_heads, dim);
 }
 
-int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int dtype, const serq_kv_cache* cache,
-                    const serq_kv_batch* batch, int max_q, int64_t max_kv, float scale, int window,
-                    void* out, int64_t ldo, int64_t ldoh, float* lse,
-                    void* workspace, size_t workspace_bytes, void* stream) {
-  AttnParams p{};
+int serq_paged_attn_mod(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int dtype, const serq_kv_cache* cache,
+                        const serq_kv_batch* batch, int max_q, int64_t max_kv, float scale, int window, const serq_attn_mod* mod,
+                        void* out, int64_t ldo, int64_t ldoh, float* lse,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  AttnModParams p{};
   int rc = kv_check(cache, batch, dtype, p.c);
   if (rc != SERQ_OK) return rc;
   const int D = cache->dim;
   if (q_heads < 1 || q_heads > 65535 || q_heads % cache->heads || window < 0 || max_q < 0 || max_kv < 0) return SERQ_ESHAPE;
   if (!counts_ok(batch->tokens, batch->seqs, q_heads, cache->heads)) return SERQ_ESHAPE;
   if (!(scale > 0.0f) || !(scale <= FLT_MAX)) return SERQ_ESHAPE;
+  if (mod) {
+    if (!(mod->cap >= 0.0f) || !(mod->cap <= SERQ_ATTN_MAX_CAP)) return SERQ_ESHAPE;
+    if (mod->cap > 0.0f && mod->slopes) return SERQ_EUNSUPPORTED;
+  }
   if (batch->tokens == 0 || batch->seqs == 0) return SERQ_OK;
   if ((rc = kv_check_rows(q, ldq, ldqh, q_heads, D)) != SERQ_OK) return rc;
   if ((rc = kv_check_rows(out, ldo, ldoh, q_heads, D)) != SERQ_OK) return rc;
   if (!kv_aligned(lse, 4) || !kv_aligned(workspace, 16)) return SERQ_EALIGN;
+  if (mod && (!kv_aligned(mod->slopes, 4) || !kv_aligned(mod->see_from, 4) || !kv_aligned(mod->see_to, 4))) return SERQ_EALIGN;
   p.q = (const char*)q; p.out = (char*)out; p.lse = lse;
   p.ldq = 2 * ldq; p.ldqh = 2 * ldqh; p.ldo = 2 * ldo; p.ldoh = 2 * ldoh;
   p.q_heads = q_heads; p.group = q_heads / cache->heads; p.window = window; p.scale = scale;
+  if (mod) {
+    p.from = mod->see_from; p.to = mod->see_to; p.slopes = mod->slopes; p.cap = mod->cap;
+  }
   const bool f8 = cache->dtype == SERQ_F8;
   // (as wide as the table or wider: it hides nothing, and the position of a token before the start less such a window would not fit 32 bits)
   if (window >= (int64_t)batch->table_width * cache->page_size) p.window = window = 0;
   if (!workspace) workspace_bytes = 0;
-  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, window, cache->heads, p.group, D, f8, workspace_bytes);
-  AttnParams few = p, many = p;
+  // (a row that sees keys behind its own may see more than a window of them)
+  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, p.to ? 0 : window, cache->heads, p.group, D, f8, workspace_bytes);
+  AttnModParams few = p, many = p;
   few.slices = k.f.slices; few.slice_keys = k.f.slice_keys;
   few.rows_from = 0; few.rows_to = k.many ? k.few_rows + 1 : 0x7fffffff;
   few.tickets = (uint32_t*)workspace;
@@ -190,9 +199,21 @@ int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int d
   many.tickets = few.tickets + kTickets;
   many.part = (float*)((char*)workspace + kTicketBytes + k.f.bytes);
   hipStream_t st = (hipStream_t)stream;
+  if (p.cap > 0.0f || p.slopes || p.from || p.to) {
+    const ModLaunch a{k.many ? &many : nullptr, k.few ? &few : nullptr, dtype, f8, D, k.nb, k.m.blocks, k.f.blocks};
+    return p.cap > 0.0f ? launch_paged_attn_capped(a, st) : p.slopes ? launch_paged_attn_biased(a, st) : launch_paged_attn_ranges(a, st);
+  }
   if (k.few && k.many && k.nb == 1) return launch_paged_attn_mixed(many, few, dtype, f8, D, k.m.blocks, k.f.blocks, st);
   if (k.many && (rc = launch_paged_attn_tile(many, dtype, f8, D, k.m.blocks, st)) != SERQ_OK) return rc;
   return k.few ? launch_paged_attn_few(few, dtype, f8, D, k.nb, k.f.blocks, st) : SERQ_OK;
+}
+
+int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int dtype, const serq_kv_cache* cache,
+                    const serq_kv_batch* batch, int max_q, int64_t max_kv, float scale, int window,
+                    void* out, int64_t ldo, int64_t ldoh, float* lse,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+  return serq_paged_attn_mod(q, ldq, ldqh, q_heads, dtype, cache, batch, max_q, max_kv, scale, window, nullptr, out, ldo, ldoh, lse, workspace,
+                             workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -59,8 +59,8 @@ template <int D>
 __device__ __forceinline__ int turned(int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); }
 
 // The slots slot(0) .. slot(ns - 1), joined in this order and written out.  scratch: rows x (ns + 1) floats of LDS.
-template <int DT, int D, int BM, int THREADS, class Slot>
-__device__ __forceinline__ void join_slices(const AttnParams& p, const RowBlock& k, int h, int ns, const Slot& slot, float* scratch, int tok0,
+template <int DT, int D, int BM, int THREADS, class P, class Slot>
+__device__ __forceinline__ void join_slices(const P& p, const RowBlock& k, int h, int ns, const Slot& slot, float* scratch, int tok0,
                                             float vs, int tid) {
   const int l = tid & 63, w = uniform(tid >> 6);
   const auto put = [&](int r, int d, const v2f& acc, float f) {
@@ -70,7 +70,7 @@ __device__ __forceinline__ void join_slices(const AttnParams& p, const RowBlock&
   };
   const auto put_lse = [&](int r, float m, float sum) {
     const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
-    if (p.lse) p.lse[(int64_t)(tok0 + i) * p.q_heads + h * p.group + g] = row_lse(m, sum);
+    if (p.lse) p.lse[(int64_t)(tok0 + i) * p.q_heads + h * p.group + g] = lse_of(p, m, sum);
   };
   // A load takes a microsecond here, so as many as can be are under way together.  Few slices: every thread computes their weights by itself
   // (past the end: the last slot again, without weight).
@@ -160,8 +160,8 @@ struct Part {
 };
 
 // Keys k0 .. k1-1 for the rows of block k and key head h.
-template <int DT, bool F8, int D, int NB>
-__device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, int h, int k0, int k1, const bool cut,
+template <int DT, bool F8, int D, int NB, int MOD>
+__device__ __forceinline__ void stretch(const ParamsOf<MOD>& p, const RowBlock& k, int h, int k0, int k1, const bool cut,
                                         const Part<16 * NB * (D + 2)> part, char* lds, float (*stat)[16 * NB][2]) {
   using S = Few<F8, D, NB>;
   constexpr int TG = S::TG, KEYS = S::KEYS, KL = S::KL, BM = 16 * NB, VL = TG * KL, OPITCH = S::OPITCH, REGION = S::REGION;
@@ -184,13 +184,25 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
   // the rows' queries, and the keys that each sees: lo <= j < hi
   u4 q[NB][S::STEPS];
   int lo[NB], hi[NB];
+  float slope[NB];                                            // biased: of the row's head; the row's position less the lane's first key
+  int place[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int r = k.r0 + 16 * nb + n16;
     const bool live = 16 * nb + n16 < k.rows;
     const int i = r / G, g = r - i * G;
-    hi[nb] = live ? min(k.L - k.n + i + 1, k.end) : 0;
-    lo[nb] = p.window > 0 ? max(0, k.L - k.n + i - p.window + 1) : 0;
+    if constexpr (MOD == kPlain) {
+      hi[nb] = live ? min(k.L - k.n + i + 1, k.end) : 0;
+      lo[nb] = p.window > 0 ? max(0, k.L - k.n + i - p.window + 1) : 0;
+    } else {
+      const Range x = live ? row_range(p, tok0 + i, k.L - k.n + i, k.L) : Range{0, 0};
+      hi[nb] = x.hi;
+      lo[nb] = x.lo;
+      if constexpr (MOD == kBiased) {
+        slope[nb] = live ? p.slopes[h * G + g] : 0.0f;
+        place[nb] = k.L - k.n + i - 4 * quad;
+      }
+    }
     const char* src = p.q + (int64_t)(tok0 + i) * p.ldq + (int64_t)(h * G + g) * p.ldqh;
 #pragma unroll
     for (int st = 0; st < S::STEPS; ++st) {
@@ -201,7 +213,10 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
   }
   const int all_lo = k.all_from, all_hi = k.all_to;           // no mask there
   const float ks = p.c.k_scale ? p.c.k_scale[h] : 1.0f, vs = p.c.v_scale ? p.c.v_scale[h] : 1.0f;
-  const float c = score_factor(p.scale, ks), slack = score_slack(c);
+  const float c = factor_of<MOD>(p, ks), slack = score_slack(c);
+  if constexpr (MOD == kBiased)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) slope[nb] = score_slope(slope[nb], c);
 
   const char* kbase = p.c.k + h * p.c.k_head;
   const char* vbase = p.c.v + h * p.c.v_head;
@@ -291,8 +306,18 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         sc[a][nb] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (MOD == kBiased) {
+          const float d = (float)(place[nb] - key0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[a][nb][e] = distance_bias(slope[nb], d - (float)(16 * a + e));
+        }
 #pragma unroll
         for (int st = 0; st < S::STEPS; ++st) sc[a][nb] = mfma<DT>(kk[st], q[nb][st], sc[a][nb]);
+        if constexpr (MOD == kCapped) {
+          const Cap capped(p, ks);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[a][nb][e] = capped(sc[a][nb][e]);
+        }
       }
     }
     if constexpr (MORE) {
@@ -351,7 +376,7 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
       if (__ballot(top > ref[nb] + slack)) {
         const float now = fmaxf(ref[nb], quads_reduce(top, [](float x, float y) { return fmaxf(x, y); }));
         ref[nb] = now;
-        const float mc = reference<DT>(now, c), f = exp2_fast(m[nb] - mc);
+        const float mc = reference_of<MOD, DT>(now, c), f = exp2_fast(m[nb] - mc);
         m[nb] = mc;
         sum[nb] *= f;
 #pragma unroll
@@ -435,7 +460,7 @@ __device__ __forceinline__ void stretch(const AttnParams& p, const RowBlock& k, 
       const float f = row_factor(all, vs);
       char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (head0 + g) * p.ldoh;
       *(u2*)(dst + 2 * d) = (u2){pack16<DT>(acc[0] * f, acc[1] * f), pack16<DT>(acc[2] * f, acc[3] * f)};
-      if (p.lse && d == 0) p.lse[(int64_t)(tok0 + i) * p.q_heads + head0 + g] = row_lse(top, all);
+      if (p.lse && d == 0) p.lse[(int64_t)(tok0 + i) * p.q_heads + head0 + g] = lse_of(p, top, all);
     }
   }
   if (!cut) return;
@@ -449,8 +474,8 @@ constexpr int kUnit = 64;                                     // keys of a piece
 
 // What workgroup `id` of `count` does.  lds: kLds bytes, 16-byte aligned.
 template <bool F8, int D, int NB> constexpr int kLds = kWaves * Few<F8, D, NB>::REGION;
-template <int DT, bool F8, int D, int NB>
-__device__ __forceinline__ void work(const AttnParams& p, int id, int count, char* lds) {
+template <int DT, bool F8, int D, int NB, int MOD = kPlain>
+__device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, int count, char* lds) {
   constexpr int BM = 16 * NB;
   __shared__ float stat[kWaves][BM][2];
   const int heads = p.c.heads;
@@ -459,12 +484,19 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, int count, cha
   if (p.slices <= 1) {                                        // nowhere to meet: a workgroup takes a sequence whole
     const int c0 = uniform(p.c.cu[number]), n = uniform(p.c.cu[number + 1]) - c0;
     if (!takes(p, c0, n)) return;
-    const RowBlock k = row_block<BM>(p, number, c0, n, uniform(p.c.len[number]), 0);
-    stretch<DT, F8, D, NB>(p, k, h, k.begin & ~15, max(k.end, 0), false, {}, lds, stat);
+    const RowBlock k = block_of<BM>(p, number, c0, n, uniform(p.c.len[number]), 0);
+    stretch<DT, F8, D, NB, MOD>(p, k, h, k.begin & ~15, max(k.end, 0), false, {}, lds, stat);
     return;
   }
   // (a sequence has one piece at least: its rows have to be written)
   const auto pieces = [&](int c0, int n, int L) {
+    if constexpr (MOD != kPlain) {                            // (what block_of finds for the same rows)
+      const int tokens = (min(n * p.group, BM) + p.group - 1) / p.group;
+      Seen s;
+      for (int i = 0; i < tokens; ++i) s.add(row_range(p, c0 + i, L - n + i, L));
+      const int base = s.begin & ~15;
+      return s.end > 0 ? (s.end - base - 1) / kUnit + 1 : 1;
+    }
     const int end = min(L, p.c.width << p.c.page_shift), base = (p.window > 0 ? max(0, L - n - p.window + 1) : 0) & ~15;
     return end > base ? (end - base - 1) / kUnit + 1 : 1;
   };
@@ -476,7 +508,7 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, int count, cha
   const int stop = min(at + share, total);
   while (at < stop) {
     const Sequence x = line.find(at);
-    const RowBlock k = row_block<BM>(p, x.b, x.c0, x.n, x.L, 0);
+    const RowBlock k = block_of<BM>(p, x.b, x.c0, x.n, x.L, 0);
     const int ends = x.before + x.pieces, until = min(stop, ends), base = k.begin & ~15;
     const bool cut = at > x.before || until < ends;
     // (a sequence of more tokens than max_q has pieces past what the block's rows see, maybe nothing that they see: no table entry is read there)
@@ -486,7 +518,7 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, int count, cha
       const int first = x.before / share;
       part = {p.part + (int64_t)h * wanted * 2 * (BM * (D + 2)), p.tickets + h * wanted + first, first, number - first, (ends - 1) / share - first + 1};
     }
-    stretch<DT, F8, D, NB>(p, k, h, k0, k1, cut, part, lds, stat);
+    stretch<DT, F8, D, NB, MOD>(p, k, h, k0, k1, cut, part, lds, stat);
     at = until;
     __syncthreads();                                          // LDS is free again
   }

@@ -1,0 +1,56 @@
+// The kernels of serq_paged_attn_mod: those of serq_paged_attn with what stands between the scores and the softmax (Mod), each compiled in a
+// source of its own (paged_attn_ranges.hip, paged_attn_capped.hip, paged_attn_biased.hip), and a call's launch.
+#pragma once
+
+#include "paged_attn_few.h"
+#include "paged_attn_tile.h"
+
+namespace serq {
+namespace {
+
+template <int DT, bool F8, int D, int NB, int MOD>
+__global__ __launch_bounds__(256, 2) void paged_attn_mod_few_kernel(AttnModParams p) {
+  __shared__ __align__(16) char lds[few::kLds<F8, D, NB>];
+  few::work<DT, F8, D, NB, MOD>(p, blockIdx.x, gridDim.x, lds);
+}
+
+template <int DT, bool F8, int D, int MOD>
+__global__ __launch_bounds__(256, 2) void paged_attn_mod_tile_kernel(AttnModParams p) {
+  __shared__ __align__(16) char lds[tile::kLds<D>];
+  tile::work<DT, F8, D, MOD>(p, blockIdx.x, lds);
+}
+
+template <int DT, bool F8, int D, int MOD>
+__global__ __launch_bounds__(256, 2) void paged_attn_mod_mixed_kernel(AttnModParams many, AttnModParams few, int tiles) {
+  constexpr int LDS = tile::kLds<D> > few::kLds<F8, D, 1> ? tile::kLds<D> : few::kLds<F8, D, 1>;
+  __shared__ __align__(16) char lds[LDS];
+  if ((int)blockIdx.x < tiles) tile::work<DT, F8, D, MOD>(many, blockIdx.x, lds);
+  else few::work<DT, F8, D, 1, MOD>(few, blockIdx.x - tiles, gridDim.x - tiles, lds);
+}
+
+template <int MOD, int DT, bool F8, int D>
+int launch_mod_of(const ModLaunch& a, hipStream_t st) {
+  const int tiles = a.many ? a.blocks * a.many->slices * a.many->c.heads : 0;
+  if (a.many && a.few && a.nb == 1) {
+    hipLaunchKernelGGL((paged_attn_mod_mixed_kernel<DT, F8, D, MOD>), dim3((unsigned)(tiles + a.shares)), dim3(256), 0, st, *a.many, *a.few, tiles);
+  } else {
+    if (a.many) hipLaunchKernelGGL((paged_attn_mod_tile_kernel<DT, F8, D, MOD>), dim3((unsigned)tiles), dim3(256), 0, st, *a.many);
+    if (a.few && a.nb == 1) hipLaunchKernelGGL((paged_attn_mod_few_kernel<DT, F8, D, 1, MOD>), dim3((unsigned)a.shares), dim3(256), 0, st, *a.few);
+    else if (a.few) hipLaunchKernelGGL((paged_attn_mod_few_kernel<DT, F8, D, 2, MOD>), dim3((unsigned)a.shares), dim3(256), 0, st, *a.few);
+  }
+  return hipGetLastError() == hipSuccess ? SERQ_OK : SERQ_EHIP;
+}
+
+template <int MOD>
+int launch_mod(const ModLaunch& a, hipStream_t st) {
+  const bool bf = a.dtype == SERQ_BF16;
+  if (a.D == 128) {
+    if (bf) return a.f8 ? launch_mod_of<MOD, SERQ_BF16, true, 128>(a, st) : launch_mod_of<MOD, SERQ_BF16, false, 128>(a, st);
+    return a.f8 ? launch_mod_of<MOD, SERQ_F16, true, 128>(a, st) : launch_mod_of<MOD, SERQ_F16, false, 128>(a, st);
+  }
+  if (bf) return a.f8 ? launch_mod_of<MOD, SERQ_BF16, true, 64>(a, st) : launch_mod_of<MOD, SERQ_BF16, false, 64>(a, st);
+  return a.f8 ? launch_mod_of<MOD, SERQ_F16, true, 64>(a, st) : launch_mod_of<MOD, SERQ_F16, false, 64>(a, st);
+}
+
+}  // namespace
+}  // namespace serq

@@ -58,8 +58,8 @@ __device__ __forceinline__ void dma_rows(const char* from, const uint32_t (&voff
 
 // What workgroup `id` does.  lds: kLds bytes, 16-byte aligned: K, then V of two tiles.
 template <int D> constexpr int kLds = 2 * 2 * kKeys * D * 2;
-template <int DT, bool F8, int D>
-__device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all) {
+template <int DT, bool F8, int D, int MOD = kPlain>
+__device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, char* lds_all) {
   constexpr int NW = kTileRows / 32, BM = kTileRows;          // waves
   constexpr int ROW = D * 2;                                  // bytes of a key in LDS
   constexpr int TILE = kKeys * ROW;                           // of K or of V
@@ -82,7 +82,7 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
   if (number >= line.total) return;
   const int block = line.total - 1 - number;
   const Sequence seq = line.find(block);
-  const RowBlock k = row_block<BM>(p, seq.b, seq.c0, seq.n, seq.L, (block - seq.before) * BM);
+  const RowBlock k = block_of<BM>(p, seq.b, seq.c0, seq.n, seq.L, (block - seq.before) * BM);
   const int base = k.begin & ~15;
   const int ns = k.end > base ? min((k.end - base - 1) / p.slice_keys + 1, p.slices) : 1;
   if (s >= ns) return;
@@ -94,7 +94,15 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
   const bool live = rin < k.rows;
   const int i = r / G, g = r - i * G;
   const int first = k.L - k.n;
-  const int hi = live ? min(first + i + 1, k.end) : 0, lo = p.window > 0 ? max(0, first + i - p.window + 1) : 0;
+  int hi, lo;
+  if constexpr (MOD == kPlain) {
+    hi = live ? min(first + i + 1, k.end) : 0;
+    lo = p.window > 0 ? max(0, first + i - p.window + 1) : 0;
+  } else {
+    const Range x = live ? row_range(p, tok0 + i, first + i, k.L) : Range{0, 0};
+    hi = x.hi;
+    lo = x.lo;
+  }
   u4 q[STEPS];
   {
     const char* src = p.q + (int64_t)(tok0 + i) * p.ldq + (int64_t)(h * G + g) * p.ldqh;
@@ -103,9 +111,31 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
   }
   // keys that all of the wave's rows see: no mask there (a wave without rows: whatever)
   const int wr0 = k.r0 + 32 * w, wr1 = min(k.r0 + k.rows, wr0 + 32) - 1;
-  const int all_lo = p.window > 0 ? max(0, first + wr1 / G - p.window + 1) : 0, all_hi = min(first + wr0 / G + 1, k.end);
+  int all_lo, all_hi;
+  if constexpr (MOD == kPlain) {
+    all_lo = p.window > 0 ? max(0, first + wr1 / G - p.window + 1) : 0;
+    all_hi = min(first + wr0 / G + 1, k.end);
+  } else {
+    all_lo = wave_max_int(live ? lo : 0);
+    all_hi = wave_min_int(live ? hi : 0x7fffffff);
+  }
   const float ks = p.c.k_scale ? p.c.k_scale[h] : 1.0f, vs = p.c.v_scale ? p.c.v_scale[h] : 1.0f;
-  const float c = score_factor(p.scale, ks), slack = score_slack(c);
+  const float c = factor_of<MOD>(p, ks), slack = score_slack(c);
+  float slope = 0.0f;                                         // biased: of the row's head; the row's position less the lane's first key
+  const int place = first + i - 4 * half;
+  if constexpr (MOD == kBiased) slope = live ? score_slope(p.slopes[h * G + g], c) : 0.0f;
+  const auto capped = [&](float s) {
+    if constexpr (MOD == kCapped) return Cap(p, ks)(s);
+    else return s;
+  };
+  // what tile t's scores begin with
+  const auto begin_scores = [&](v16f (&sc)[2], int t) {
+    const float d = MOD == kBiased ? (float)(place - (k0 + t * kKeys)) : 0.0f;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[kb][e] = MOD == kBiased ? distance_bias(slope, d - (float)(32 * kb + 8 * (e / 4) + e % 4)) : 0.0f;
+  };
 
   // ---- loads: a wave brings LOADS * RPI rows of K and of V, which lie in one page
   const int mask = (1 << p.c.page_shift) - 1;
@@ -259,7 +289,7 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
       const uint32_t bits = __float_as_uint(top);
       const auto two = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
       ref = fmaxf(ref, fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])));
-      const float mc = reference<DT>(ref, c), f = exp2_fast(m - mc);
+      const float mc = reference_of<MOD, DT>(ref, c), f = exp2_fast(m - mc);
       m = mc;
       sum *= f;
       sum2 *= f;
@@ -270,10 +300,7 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
     }
     // the next tile's scores, and this one's weights, two a time
     u4 pw[4], vf[2][DB];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) next[kb][e] = 0.0f;
+    begin_scores(next, t + 1);
     // (the wave that is here goes before the other one of the SIMD, which is most often at its products with V: see the figures above)
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -302,6 +329,10 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
         if (g < 3) vf[(g + 1) & 1][d] = v_piece(t, g + 1, d);
         if constexpr (MORE) {                                 // the next tile's largest score, some of them a time
           const int n = g * DB + d;
+          if constexpr (MOD == kCapped) {
+#pragma unroll
+            for (int e = n * 32 / (4 * DB); e < (n + 1) * 32 / (4 * DB); ++e) next[e / 16][e % 16] = capped(next[e / 16][e % 16]);
+          }
           if (n == 0) top = next[0][0];
 #pragma unroll
           for (int e = n * 32 / (4 * DB); e < (n + 1) * 32 / (4 * DB); ++e) top = fmaxf(top, next[e / 16][e % 16]);
@@ -325,12 +356,13 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sa[kb][e] = 0.0f;
+    begin_scores(sa, 0);
 #pragma unroll
     for (int i = 0; i < QK; ++i) sa[i / STEPS] = mfma<DT>(k_piece(0, i), q[i % STEPS], sa[i / STEPS]);
+    if constexpr (MOD == kCapped) {
+#pragma unroll
+      for (int e = 0; e < 32; ++e) sa[e / 16][e % 16] = capped(sa[e / 16][e % 16]);
+    }
     top = largest(sa);
     int t = 0;
     for (; t + 2 < nt; t += 2) {
@@ -408,7 +440,7 @@ __device__ __forceinline__ void work(const AttnParams& p, int id, char* lds_all)
     for (int e = 0; e < 4; ++e)
       *(u2*)(dst + 2 * (32 * d + 8 * e + 4 * half)) = (u2){pack16<DT>(o[d][4 * e] * f, o[d][4 * e + 1] * f),
                                                            pack16<DT>(o[d][4 * e + 2] * f, o[d][4 * e + 3] * f)};
-  if (p.lse && half == 0) p.lse[(int64_t)(tok0 + i) * p.q_heads + h * G + g] = row_lse(m, all);
+  if (p.lse && half == 0) p.lse[(int64_t)(tok0 + i) * p.q_heads + h * G + g] = lse_of(p, m, all);
 }
 
 }  // namespace tile

@@ -64,7 +64,7 @@ def test_binding_refuses():
         with pytest.raises(TypeError):
             f(x)
     with pytest.raises(ValueError):
-        serq._fast.bind_norm(0, 0, 0, 0)
+        serq._fast.bind_norm(0, 0, 0, 0, 0)
 
 
 def test_oracle_by_hand():
