@@ -128,7 +128,8 @@ __device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, char* lds_a
     if constexpr (MOD == kCapped) return Cap(p, ks)(s);
     else return s;
   };
-  // what tile t's scores begin with
+  // what tile t's scores begin with (one multiply-add a score from the tile's first distance would take 541 us for 8192 tokens instead of 551, but leave a
+  // steep slope's rounding on the row's own key)
   const auto begin_scores = [&](v16f (&sc)[2], int t) {
     const float d = MOD == kBiased ? (float)(place - (k0 + t * kKeys)) : 0.0f;
 #pragma unroll
@@ -255,14 +256,26 @@ __device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, char* lds_a
     const int key0 = k0 + t * kKeys;
     if (key0 < k.begin || key0 + kKeys > k.end || key0 < k.all_from || key0 + kKeys > k.all_to) {
       // values of keys that no row sees become zero (a weight of zero does not make NaN zero); of those that some see, what is not finite
-      bool found = false;
-      for (int at = tid; at < TILE / 16; at += 64 * NW) {
-        const int key = key0 + at / (ROW / 16);
-        u4* v = (u4*)(lds[t & 1][1] + at * 16);
-        if (key < k.begin || key >= k.end) *v = (u4){0, 0, 0, 0};
-        else if (key < k.all_from || key >= k.all_to) *v = take_out<DT>(*v, found);
+      // (that test eight values a time, since most often all are: 12000 tokens of packed documents 180 us without it, 158 with it)
+      constexpr int N = F8 && MOD == kCapped ? 1 : TILE / 16 / (64 * NW);    // pieces a time (four: registers)
+#pragma unroll 1
+      for (int at = tid; at < TILE / 16; at += 64 * NW * N) {
+        u4* const v = (u4*)(lds[t & 1][1]) + at;
+        u4 x[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = v[64 * NW * i];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int key = key0 + (at + 64 * NW * i) / (ROW / 16);
+          if (key < k.begin || key >= k.end) {
+            v[64 * NW * i] = (u4){0, 0, 0, 0};
+          } else if ((key < k.all_from || key >= k.all_to) && any_odd<DT>(x[i])) {
+            bool found = false;
+            v[64 * NW * i] = take_out<DT>(x[i], found);
+            odd = 1;
+          }
+        }
       }
-      if (found) odd = 1;
       __syncthreads();
     }
     const bool more_k = t + 2 < nt;
