@@ -37,10 +37,13 @@ constexpr size_t kManyRoom = 46u << 20;                        // most that its 
 
 // The kernel for many rows: blocks of rows times key heads are the workgroups; where they would leave compute units idle, the keys (at most `keys` that
 // a row block sees) are cut into slices.  Taken is the number of slices with the shortest time.  A tile of 64 keys takes a workgroup 1.08 us on a
-// compute unit of its own, 1.85 beside another; to begin takes 5 us, to begin and to meet 8 and one a slice.  `blocks` counts a block more for each
+// compute unit of its own, 1.85 beside another; to begin takes 5 of these, to begin and to meet 8 and one a slice.  Where some units have one workgroup and some
+// two, what has no partner is done sooner and begins and ends hide behind the partner's work.  `blocks` counts a block more for each
 // sequence than may be needed (every sequence's last one is half empty on average); `full` is about what there is.
 // Measured (32 query and 8 key heads; us with 1 / 2 / 3 / 4 / 5 / 8 slices): 384 tokens after 3500 66.6 / 43.1 / 44.8 / 45.5 / 45.2 / 48.4, 100 after 30000
 // 469 / 245 / 171 / 134 / 114 / 87, 512 fresh ones 14.9 / 16.9 / 17.3 / 21.5; 512 after 32000 with 2 / 4 292 / 272, 256 after 8000 with 3 / 4 56.5 / 50.6.
+// With 1 / 2 / 3 / 4: 700 after 2500 56.9 / 52.2 / 56.7 / 68.5 (E4M3 73.5 / 64.3 / 63.9 / 74.1), beside 7 single tokens 65.7 / 55.7 / 66.7 / 62.7; 600 after
+// 6000 109 / 85.5 / 75.7 / 98.8; 512 after 4000 77.0 / 51.3 / 54.3 / 53.3.
 constexpr int64_t kGrain = 128;                                // keys of a slice are a multiple of it
 Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, size_t slot_floats, size_t room) {
   Plan k{blocks, 1, 0x7fffff00, 0};
@@ -51,8 +54,10 @@ Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, s
     const int64_t each = ((keys + n - 1) / n + kGrain - 1) / kGrain * kGrain;
     if ((keys + each - 1) / each != n) continue;
     const double a_unit = (double)(full * heads * n) / (double)cus;
-    const double slow = a_unit <= 1.0 ? 1.08 : a_unit <= 2.0 ? 1.85 : 0.93 * a_unit + 0.4;
-    const double time = slow * (double)((each + 63) / 64 + (n > 1 ? 8 + n : 5));
+    const double tiles = (double)((each + 63) / 64), ends = n > 1 ? 8.0 + (double)n : 5.0;
+    const double time = a_unit <= 1.0   ? 1.08 * (tiles + ends)
+                        : a_unit <= 2.0 ? (1.25 + 0.3 * a_unit) * tiles + (1.2 * a_unit - 0.6) * ends
+                                        : (0.93 * a_unit + 0.4) * (tiles + ends);
     if (n == 1 || time < 0.95 * least) {
       least = time;
       k.slices = (int)n;
