@@ -112,10 +112,12 @@ Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int
     const int64_t slots = (int64_t)few_slots_bytes(1, heads, k.nb, D);                    // bytes of a workgroup for each head
     // Where a sequence's parts and rows are many, a workgroup for every compute unit: half as many slots meet, and a unit streams as fast alone.  Measured (us,
     // as many as run together / one a unit, 8 key heads): 1 token over 131000 88.3 / 84.3, over 32000 32.8 / 29.9, 8 over 130000 134.9 / 115.9, 4 of 8
-    // tokens over 8000 53.5 / 44.4; one token each of 255 sequences of up to 2000 157 / 163.
+    // tokens over 8000 53.5 / 44.4; one token each of 255 sequences of up to 2000 157 / 163. A sequence alone has no other whose start could hide behind
+    // its work: one token, 16 heads of 64 channels over 8000 13.7 / 12.8, over 65000 48.0 / 46.0, 8 heads of 128 over 32000 29.5 / 27.2 (four sequences of up to
+    // 12000, 16 heads: 24.0 / 27.2).
     const int64_t rows_few = rows <= k.few_rows ? rows : group;
     int64_t each = (together + heads - 1) / heads;
-    each = few_shares(seqs > 0 && each / seqs * rows_few >= 256 ? cus : together, seqs, heads, keys);
+    each = few_shares(seqs == 1 || (seqs > 0 && each / seqs * rows_few >= 256) ? cus : together, seqs, heads, keys);
     if (each > (int64_t)room / slots) each = (int64_t)room / slots;
     k.f = Plan{(int)whole, 1, 0, 0};
     if (whole * 256 < keys * together && each > 0) k.f = Plan{(int)each * heads, 2, (int)few_keys(rows_few, keys), (size_t)(each * slots)};
