@@ -139,7 +139,12 @@ size_t most_bytes(int64_t tokens, int seqs, int max_q, int64_t max_kv, int heads
   if (max_kv > kKvPositions) max_kv = kKvPositions;
   const int nb = rows > 16 ? 2 : 1;
   const int resident = nb > 1 ? paged_attn_few_resident(nb, false, D) : paged_attn_few_resident(nb, true, D);   // (the larger one: E4M3)
-  size_t bytes = kTicketBytes + few_slots_bytes(few_shares(cus * resident, seqs, heads, max_kv), heads, nb, D);
+  size_t bytes = few_slots_bytes(few_shares(cus * resident, seqs, heads, max_kv), heads, nb, D);
+  if (D == 64 && heads % 2 == 0 && 2 * rows <= 16) {           // (two heads a time)
+    const size_t pairs = few_slots_bytes(few_shares(cus * paged_attn_few_resident(1, false, 128), seqs, heads / 2, max_kv), heads / 2, 1, 128);
+    if (pairs > bytes) bytes = pairs;
+  }
+  bytes += kTicketBytes;
   if (rows > 32 && max_kv > kGrain) {
     int64_t units = (int64_t)many_blocks(tokens, seqs, group) * heads, slices = (max_kv + kGrain - 1) / kGrain;
     if (units > kTickets) units = kTickets;
@@ -194,8 +199,18 @@ int serq_paged_attn_mod(const void* q, int64_t ldq, int64_t ldqh, int q_heads, i
   // (as wide as the table or wider: it hides nothing, and the position of a token before the start less such a window would not fit 32 bits)
   if (window >= (int64_t)batch->table_width * cache->page_size) p.window = window = 0;
   if (!workspace) workspace_bytes = 0;
+  // narrow heads side by side in memory: two a time, where both heads' rows fit the kernel for few
+  int64_t rows = max_q < batch->tokens ? max_q : batch->tokens;
+  rows *= p.group;
+  const bool pairs = !f8 && D == 64 && cache->heads % 2 == 0 && cache->k_head == 64 && cache->v_head == 64 && 2 * rows <= 16;
+  if (pairs) {
+    p.c.heads /= 2;
+    p.c.k_head *= 2;
+    p.c.v_head *= 2;
+    p.group *= 2;
+  }
   // (a row that sees keys behind its own may see more than a window of them)
-  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, p.to ? 0 : window, cache->heads, p.group, D, f8, workspace_bytes);
+  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, p.to ? 0 : window, p.c.heads, p.group, pairs ? 128 : D, f8, workspace_bytes);
   AttnModParams few = p, many = p;
   few.slices = k.f.slices; few.slice_keys = k.f.slice_keys;
   few.rows_from = 0; few.rows_to = k.many ? k.few_rows + 1 : 0x7fffffff;
@@ -207,12 +222,12 @@ int serq_paged_attn_mod(const void* q, int64_t ldq, int64_t ldqh, int q_heads, i
   many.part = (float*)((char*)workspace + kTicketBytes + k.f.bytes);
   hipStream_t st = (hipStream_t)stream;
   if (p.cap > 0.0f || p.slopes || p.from || p.to) {
-    const ModLaunch a{k.many ? &many : nullptr, k.few ? &few : nullptr, dtype, f8, D, k.nb, k.m.blocks, k.f.blocks};
+    const ModLaunch a{k.many ? &many : nullptr, k.few ? &few : nullptr, dtype, f8, D, k.nb, k.m.blocks, k.f.blocks, pairs};
     return p.cap > 0.0f ? launch_paged_attn_capped(a, st) : p.slopes ? launch_paged_attn_biased(a, st) : launch_paged_attn_ranges(a, st);
   }
   if (k.few && k.many && k.nb == 1) return launch_paged_attn_mixed(many, few, dtype, f8, D, k.m.blocks, k.f.blocks, st);
   if (k.many && (rc = launch_paged_attn_tile(many, dtype, f8, D, k.m.blocks, st)) != SERQ_OK) return rc;
-  return k.few ? launch_paged_attn_few(few, dtype, f8, D, k.nb, k.f.blocks, st) : SERQ_OK;
+  return k.few ? launch_paged_attn_few(few, dtype, f8, D, k.nb, pairs, k.f.blocks, st) : SERQ_OK;
 }
 
 int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int dtype, const serq_kv_cache* cache,

@@ -54,19 +54,25 @@ __device__ __forceinline__ v4f mfma(const u4& a, const u4& b, const v4f& c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
 }
 
+// PAIRS: two neighbouring key heads of 64 channels, side by side in memory, are read as one of 128.  The queries of both are its rows, with zeros for the
+// other's channels; of a row's scores and of its sums the other's are dropped.  (A head's 128 bytes out of rows of 2 KiB come slowly: one token, 16 heads over 65000
+// keys, by [page, row, head] 60.7 us against 46 by [page, head, row].)
+template <bool PAIRS>
+__device__ __forceinline__ bool own_half(int g, int group, int d) { return !PAIRS || (d >= 64) == (2 * g >= group); }
+
 // rows of V in LDS: 16-byte pieces, their place turned by the row so that 8 rows' equal pieces lie in different banks
 template <int D>
 __device__ __forceinline__ int turned(int row) { return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); }
 
 // The slots slot(0) .. slot(ns - 1), joined in this order and written out.  scratch: rows x (ns + 1) floats of LDS.
-template <int DT, int D, int BM, int THREADS, class P, class Slot>
+template <int DT, int D, int BM, int THREADS, bool PAIRS, class P, class Slot>
 __device__ __forceinline__ void join_slices(const P& p, const RowBlock& k, int h, int ns, const Slot& slot, float* scratch, int tok0,
                                             float vs, int tid) {
   const int l = tid & 63, w = uniform(tid >> 6);
   const auto put = [&](int r, int d, const v2f& acc, float f) {
     const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
     char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (int64_t)(h * p.group + g) * p.ldoh;
-    *(uint32_t*)(dst + 2 * d) = pack16<DT>(acc[0] * f, acc[1] * f);
+    if (own_half<PAIRS>(g, p.group, d)) *(uint32_t*)(dst + 2 * (PAIRS ? d & 63 : d)) = pack16<DT>(acc[0] * f, acc[1] * f);
   };
   const auto put_lse = [&](int r, float m, float sum) {
     const int i = (k.r0 + r) / p.group, g = k.r0 + r - i * p.group;
@@ -160,7 +166,7 @@ struct Part {
 };
 
 // Keys k0 .. k1-1 for the rows of block k and key head h.
-template <int DT, bool F8, int D, int NB, int MOD>
+template <int DT, bool F8, int D, int NB, int MOD, bool PAIRS>
 __device__ __forceinline__ void stretch(const ParamsOf<MOD>& p, const RowBlock& k, int h, int k0, int k1, const bool cut,
                                         const Part<16 * NB * (D + 2)> part, char* lds, float (*stat)[16 * NB][2]) {
   using S = Few<F8, D, NB>;
@@ -186,11 +192,13 @@ __device__ __forceinline__ void stretch(const ParamsOf<MOD>& p, const RowBlock& 
   int lo[NB], hi[NB];
   float slope[NB];                                            // biased: of the row's head; the row's position less the lane's first key
   int place[NB];
+  bool second[NB];                                            // pairs: the row is of the second head
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int r = k.r0 + 16 * nb + n16;
     const bool live = 16 * nb + n16 < k.rows;
     const int i = r / G, g = r - i * G;
+    second[nb] = PAIRS && 2 * g >= G;
     if constexpr (MOD == kPlain) {
       hi[nb] = live ? min(k.L - k.n + i + 1, k.end) : 0;
       lo[nb] = p.window > 0 ? max(0, k.L - k.n + i - p.window + 1) : 0;
@@ -208,7 +216,8 @@ __device__ __forceinline__ void stretch(const ParamsOf<MOD>& p, const RowBlock& 
     for (int st = 0; st < S::STEPS; ++st) {
       // channels of step st that quad has: where its loads of K put them
       const int at = F8 ? 64 * (st / 2) + 16 * quad + 8 * (st & 1) : 32 * st + 8 * quad;
-      q[nb][st] = live ? *(const u4*)(src + 2 * at) : (u4){0, 0, 0, 0};
+      if constexpr (PAIRS) q[nb][st] = live && own_half<true>(g, G, at) ? *(const u4*)(src + 2 * (at & 63)) : (u4){0, 0, 0, 0};
+      else q[nb][st] = live ? *(const u4*)(src + 2 * at) : (u4){0, 0, 0, 0};
     }
   }
   const int all_lo = k.all_from, all_hi = k.all_to;           // no mask there
@@ -311,8 +320,19 @@ __device__ __forceinline__ void stretch(const ParamsOf<MOD>& p, const RowBlock& 
 #pragma unroll
           for (int e = 0; e < 4; ++e) sc[a][nb][e] = distance_bias(slope[nb], d - (float)(16 * a + e));
         }
+        if constexpr (PAIRS) {                                // a sum for each head, and the row's own of them: nothing of the other's keys, NaN among it, in it
+          v4f upper = sc[a][nb];
 #pragma unroll
-        for (int st = 0; st < S::STEPS; ++st) sc[a][nb] = mfma<DT>(kk[st], q[nb][st], sc[a][nb]);
+          for (int st = 0; st < S::STEPS / 2; ++st) {
+            sc[a][nb] = mfma<DT>(kk[st], q[nb][st], sc[a][nb]);
+            upper = mfma<DT>(kk[S::STEPS / 2 + st], q[nb][S::STEPS / 2 + st], upper);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[a][nb][e] = second[nb] ? upper[e] : sc[a][nb][e];
+        } else {
+#pragma unroll
+          for (int st = 0; st < S::STEPS; ++st) sc[a][nb] = mfma<DT>(kk[st], q[nb][st], sc[a][nb]);
+        }
         if constexpr (MOD == kCapped) {
           const Cap capped(p, ks);
 #pragma unroll
@@ -459,7 +479,8 @@ __device__ __forceinline__ void stretch(const ParamsOf<MOD>& p, const RowBlock& 
       const int i = (k.r0 + r) / G, g = k.r0 + r - i * G;
       const float f = row_factor(all, vs);
       char* dst = p.out + (int64_t)(tok0 + i) * p.ldo + (head0 + g) * p.ldoh;
-      *(u2*)(dst + 2 * d) = (u2){pack16<DT>(acc[0] * f, acc[1] * f), pack16<DT>(acc[2] * f, acc[3] * f)};
+      if (own_half<PAIRS>(g, G, d))
+        *(u2*)(dst + 2 * (PAIRS ? d & 63 : d)) = (u2){pack16<DT>(acc[0] * f, acc[1] * f), pack16<DT>(acc[2] * f, acc[3] * f)};
       if (p.lse && d == 0) p.lse[(int64_t)(tok0 + i) * p.q_heads + head0 + g] = lse_of(p, top, all);
     }
   }
@@ -467,14 +488,14 @@ __device__ __forceinline__ void stretch(const ParamsOf<MOD>& p, const RowBlock& 
   __shared__ uint32_t last;
   if (!last_to_arrive(part.ticket, part.count, tid, &last)) return;
   static_assert(BM * (kMaxSlices + 1) * 4 <= kWaves * REGION, "the stretches' weights");
-  join_slices<DT, D, BM, 256>(p, k, h, part.count, [&](int u) { return part.slot(u); }, (float*)lds, tok0, vs, tid);   // (the regions of the waves are free)
+  join_slices<DT, D, BM, 256, PAIRS>(p, k, h, part.count, [&](int u) { return part.slot(u); }, (float*)lds, tok0, vs, tid);   // (the regions of the waves are free)
 }
 
 constexpr int kUnit = 64;                                     // keys of a piece of a line
 
 // What workgroup `id` of `count` does.  lds: kLds bytes, 16-byte aligned.
 template <bool F8, int D, int NB> constexpr int kLds = kWaves * Few<F8, D, NB>::REGION;
-template <int DT, bool F8, int D, int NB, int MOD = kPlain>
+template <int DT, bool F8, int D, int NB, int MOD = kPlain, bool PAIRS = false>
 __device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, int count, char* lds) {
   constexpr int BM = 16 * NB;
   __shared__ float stat[kWaves][BM][2];
@@ -485,7 +506,7 @@ __device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, int count, 
     const int c0 = uniform(p.c.cu[number]), n = uniform(p.c.cu[number + 1]) - c0;
     if (!takes(p, c0, n)) return;
     const RowBlock k = block_of<BM>(p, number, c0, n, uniform(p.c.len[number]), 0);
-    stretch<DT, F8, D, NB, MOD>(p, k, h, k.begin & ~15, max(k.end, 0), false, {}, lds, stat);
+    stretch<DT, F8, D, NB, MOD, PAIRS>(p, k, h, k.begin & ~15, max(k.end, 0), false, {}, lds, stat);
     return;
   }
   // (a sequence has one piece at least: its rows have to be written)
@@ -518,7 +539,7 @@ __device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, int count, 
       const int first = x.before / share;
       part = {p.part + (int64_t)h * wanted * 2 * (BM * (D + 2)), p.tickets + h * wanted + first, first, number - first, (ends - 1) / share - first + 1};
     }
-    stretch<DT, F8, D, NB, MOD>(p, k, h, k0, k1, cut, part, lds, stat);
+    stretch<DT, F8, D, NB, MOD, PAIRS>(p, k, h, k0, k1, cut, part, lds, stat);
     at = until;
     __syncthreads();                                          // LDS is free again
   }

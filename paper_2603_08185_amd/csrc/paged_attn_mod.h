@@ -28,6 +28,12 @@ __global__ __launch_bounds__(256, 2) void paged_attn_mod_mixed_kernel(AttnModPar
   else few::work<DT, F8, D, 1, MOD>(few, blockIdx.x - tiles, gridDim.x - tiles, lds);
 }
 
+template <int DT, int MOD>
+__global__ __launch_bounds__(256, 2) void paged_attn_mod_few_pairs_kernel(AttnModParams p) {
+  __shared__ __align__(16) char lds[few::kLds<false, 128, 1>];
+  few::work<DT, false, 128, 1, MOD, true>(p, blockIdx.x, gridDim.x, lds);
+}
+
 template <int MOD, int DT, bool F8, int D>
 int launch_mod_of(const ModLaunch& a, hipStream_t st) {
   const int tiles = a.many ? a.blocks * a.many->slices * a.many->c.heads : 0;
@@ -44,6 +50,11 @@ int launch_mod_of(const ModLaunch& a, hipStream_t st) {
 template <int MOD>
 int launch_mod(const ModLaunch& a, hipStream_t st) {
   const bool bf = a.dtype == SERQ_BF16;
+  if (a.pairs) {
+    if (bf) hipLaunchKernelGGL((paged_attn_mod_few_pairs_kernel<SERQ_BF16, MOD>), dim3((unsigned)a.shares), dim3(256), 0, st, *a.few);
+    else hipLaunchKernelGGL((paged_attn_mod_few_pairs_kernel<SERQ_F16, MOD>), dim3((unsigned)a.shares), dim3(256), 0, st, *a.few);
+    return hipGetLastError() == hipSuccess ? SERQ_OK : SERQ_EHIP;
+  }
   if (a.D == 128) {
     if (bf) return a.f8 ? launch_mod_of<MOD, SERQ_BF16, true, 128>(a, st) : launch_mod_of<MOD, SERQ_BF16, false, 128>(a, st);
     return a.f8 ? launch_mod_of<MOD, SERQ_F16, true, 128>(a, st) : launch_mod_of<MOD, SERQ_F16, false, 128>(a, st);

@@ -230,3 +230,47 @@ def test_both_ways_from_python(monkeypatch):
                 _run(B, **kw)
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("mod", ["none", "cap", "bias", "wild", "bias prefix"])
+@pytest.mark.parametrize("Hq,Hkv", [(2, 2), (6, 6), (16, 4), (32, 8), (8, 1), (12, 4)])
+def test_narrow_heads_side_by_side(mod, Hq, Hkv):
+    """Heads of 64 channels next to one another in memory are read two a time: none sees the other's keys or values, NaN and infinities among them."""
+    for dt in (torch.bfloat16, torch.float16):
+        for seqs in ([(1, 700), (1, 40), (0, 3), (1, 1)], [(2, 90), (1, 300)], [(1, 5000)]):
+            kw = dict(MODS[mod]) if mod != "none" else {}
+            B = ModBatch(seqs, Hq, Hkv, 64, 16, dt, seed=Hq, order="nhd", extra=1, **kw)
+            assert B.K.stride(2) == 64
+            for ws in (None, True):                                # (with the workspace last: what follows is compared with it bit by bit)
+                clean, lse = _run(B, ws)
+                check_mod(B, clean, lse, what=f"{seqs}")
+                assert (clean[B.cu[-1]:] == 7).all()
+            if Hkv < 2:
+                continue
+            K, V, G = B.K.clone(), B.V.clone(), Hq // Hkv
+            for bad in (float("nan"), float("inf")):
+                B.K[:, :, 1::2], B.V[:, :, 0::2] = bad, bad       # odd heads' keys, even heads' values: every head has something of its own spoilt
+                out, l2 = _run(B)
+                for h in range(0, Hkv, 2):                         # an even head's softmax does not change
+                    a, b = l2[:, h * G:(h + 1) * G], lse[:, h * G:(h + 1) * G]
+                    assert torch.equal(a, b)
+                B.K.copy_(K)
+                B.V.copy_(V)
+                B.V[:, :, 1::2] = bad
+                out, _ = _run(B)
+                for h in range(0, Hkv, 2):
+                    assert torch.equal(out[:, h * G:(h + 1) * G], clean[:, h * G:(h + 1) * G])
+                B.V.copy_(V)
+
+
+def test_narrow_heads_other_strides():
+    """Keys side by side and values not, a gap between heads, an odd number of heads: heads one a time, the same results within the bounds."""
+    for Hkv, where in ((4, "gap"), (4, "values"), (3, "odd")):
+        B = ModBatch([(1, 300), (1, 77)], 2 * Hkv, Hkv, 64, 16, seed=3, cap=9.0)
+        if where != "odd":
+            for name in (("K", "V") if where == "gap" else ("V",)):
+                x = getattr(B, name)
+                wide = torch.full((*x.shape[:2], Hkv, 72), float("nan"), dtype=x.dtype, device=DEV)
+                wide[..., :64] = x
+                setattr(B, name, wide[..., :64])
+        check_mod(B, *_run(B), what=where)
