@@ -239,8 +239,6 @@ __device__ __forceinline__ u2 lds_column4(const char* p) {
   return __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p));
 }
 
-// Values of keys that some rows of a block see and others do not.  A weight of zero does not make NaN or infinity zero, so in the tiles that hold such keys
-// what is not finite is taken out before the products, and added at the end for the rows that do see it.
 // whether any of 8 values is not finite: its exponent's bits are all ones, so that one more of the lowest runs into the sign's place
 template <int DT>
 __device__ __forceinline__ bool any_odd(const u4& x) {
@@ -250,6 +248,9 @@ __device__ __forceinline__ bool any_odd(const u4& x) {
   for (int i = 0; i < 4; ++i) m |= (x[i] & 0x7fff7fffu) + STEP;
   return (m & 0x80008000u) != 0;
 }
+
+// Values of keys that some rows of a block see and others do not.  A weight of zero does not make NaN or infinity zero, so in the tiles that hold such keys
+// what is not finite is taken out before the products, and added at the end for the rows that do see it.
 template <int DT>
 __device__ __forceinline__ u4 take_out(u4 x, bool& odd) {
   constexpr uint32_t M = DT == SERQ_BF16 ? 0x7f80u : 0x7c00u;
