@@ -274,3 +274,43 @@ def test_narrow_heads_other_strides():
                 wide[..., :64] = x
                 setattr(B, name, wide[..., :64])
         check_mod(B, *_run(B), what=where)
+
+
+def test_pages_far_apart():
+    """Pages 4 GiB apart: offsets past 32 bits, heads one and two at a time, few rows and many."""
+    for Hq, Hkv, seqs in ((4, 2, [(1, 40), (2, 20)]), (8, 1, [(40, 48)])):
+        B = ModBatch(seqs, Hq, Hkv, 64, 16, seed=5, cap=6.0, ranges=prefix)
+        clean, lse = _run(B)
+        far = []
+        for x in (B.K, B.V):
+            apart = 1 << 31                                        # elements
+            wide = torch.empty(apart * (B.pages - 1) + 16 * Hkv * 64, dtype=x.dtype, device=DEV).as_strided(x.shape, (apart, Hkv * 64, 64, 1))
+            wide.copy_(x)
+            far.append(wide)
+        B.K, B.V = far
+        out, l2 = _run(B)
+        assert torch.equal(out, clean) and torch.equal(l2, lse)
+        check_mod(B, out, l2)
+
+
+def test_another_stream():
+    for mod in ("cap", "bias", "docs"):
+        B = ModBatch(SETS["long"], 8, 2, 128, 16, seed=6, **MODS[mod])
+        st = torch.cuda.Stream()
+        st.wait_stream(torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            out, lse = _run(B)
+        st.synchronize()
+        check_mod(B, out, lse, what=mod)
+
+
+def test_one_workspace_for_all_kinds():
+    """Plain and modified calls of several shapes, one after the other on the same workspace, sized for the largest."""
+    Bs = [ModBatch(SETS[n], 4, 2, 64, 16, seed=i, **MODS[m]) for i, (n, m) in enumerate((("long", "cap"), ("ones", "bias"), ("chunk", "docs"), ("few", "wild"), ("ones", "cap")))]
+    most = [max(f(B) for B in Bs) for f in (lambda B: B.T, lambda B: len(B.seqs), lambda B: B.max_q, lambda B: B.max_kv)]
+    ws = serq.paged_attention_workspace(*most, 4, 2, 64, DEV)
+    for B in Bs + Bs[::-1]:
+        plain = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, ws=ws)
+        assert plain.shape == B.q.shape
+        check_mod(B, *_run(B, ws))
