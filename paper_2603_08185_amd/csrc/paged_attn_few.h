@@ -222,7 +222,7 @@ __device__ __forceinline__ void stretch(const ParamsOf<MOD>& p, const RowBlock& 
   }
   const int all_lo = k.all_from, all_hi = k.all_to;           // no mask there
   const float ks = p.c.k_scale ? p.c.k_scale[h] : 1.0f, vs = p.c.v_scale ? p.c.v_scale[h] : 1.0f;
-  const float c = factor_of<MOD>(p, ks), slack = score_slack(c);
+  const float c = factor_of<MOD>(p, ks), slack = score_slack(c), rate = cap_rate<MOD>(p, ks);
   if constexpr (MOD == kBiased)
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) slope[nb] = score_slope(slope[nb], c);
@@ -334,9 +334,8 @@ __device__ __forceinline__ void stretch(const ParamsOf<MOD>& p, const RowBlock& 
           for (int st = 0; st < S::STEPS; ++st) sc[a][nb] = mfma<DT>(kk[st], q[nb][st], sc[a][nb]);
         }
         if constexpr (MOD == kCapped) {
-          const Cap capped(p, ks);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sc[a][nb][e] = capped(sc[a][nb][e]);
+          for (int e = 0; e < 4; ++e) sc[a][nb][e] = capped(sc[a][nb][e], rate);
         }
       }
     }
@@ -512,11 +511,13 @@ __device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, int count, 
   // (a sequence has one piece at least: its rows have to be written)
   const auto pieces = [&](int c0, int n, int L) {
     if constexpr (MOD != kPlain) {                            // (what block_of finds for the same rows)
-      const int tokens = (min(n * p.group, BM) + p.group - 1) / p.group;
-      Seen s;
-      for (int i = 0; i < tokens; ++i) s.add(row_range(p, c0 + i, L - n + i, L));
-      const int base = s.begin & ~15;
-      return s.end > 0 ? (s.end - base - 1) / kUnit + 1 : 1;
+      if (kLookAlways<BM> || p.from || p.to) {
+        const int tokens = (min(n * p.group, BM) + p.group - 1) / p.group;
+        Seen s;
+        for (int i = 0; i < tokens; ++i) s.add(row_range(p, c0 + i, L - n + i, L));
+        const int base = s.begin & ~15;
+        return s.end > 0 ? (s.end - base - 1) / kUnit + 1 : 1;
+      }
     }
     const int end = min(L, p.c.width << p.c.page_shift), base = (p.window > 0 ? max(0, L - n - p.window + 1) : 0) & ~15;
     return end > base ? (end - base - 1) / kUnit + 1 : 1;

@@ -120,14 +120,10 @@ __device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, char* lds_a
     all_hi = wave_min_int(live ? hi : 0x7fffffff);
   }
   const float ks = p.c.k_scale ? p.c.k_scale[h] : 1.0f, vs = p.c.v_scale ? p.c.v_scale[h] : 1.0f;
-  const float c = factor_of<MOD>(p, ks), slack = score_slack(c);
+  const float c = factor_of<MOD>(p, ks), slack = score_slack(c), rate = cap_rate<MOD>(p, ks);
   float slope = 0.0f;                                         // biased: of the row's head; the row's position less the lane's first key
   const int place = first + i - 4 * half;
   if constexpr (MOD == kBiased) slope = live ? score_slope(p.slopes[h * G + g], c) : 0.0f;
-  const auto capped = [&](float s) {
-    if constexpr (MOD == kCapped) return Cap(p, ks)(s);
-    else return s;
-  };
   // what tile t's scores begin with (one multiply-add a score from the tile's first distance would take 541 us for 8192 tokens instead of 551, but leave a
   // steep slope's rounding on the row's own key)
   const auto begin_scores = [&](v16f (&sc)[2], int t) {
@@ -344,7 +340,7 @@ __device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, char* lds_a
           const int n = g * DB + d;
           if constexpr (MOD == kCapped) {
 #pragma unroll
-            for (int e = n * 32 / (4 * DB); e < (n + 1) * 32 / (4 * DB); ++e) next[e / 16][e % 16] = capped(next[e / 16][e % 16]);
+            for (int e = n * 32 / (4 * DB); e < (n + 1) * 32 / (4 * DB); ++e) next[e / 16][e % 16] = capped(next[e / 16][e % 16], rate);
           }
           if (n == 0) top = next[0][0];
 #pragma unroll
@@ -374,7 +370,7 @@ __device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, char* lds_a
     for (int i = 0; i < QK; ++i) sa[i / STEPS] = mfma<DT>(k_piece(0, i), q[i % STEPS], sa[i / STEPS]);
     if constexpr (MOD == kCapped) {
 #pragma unroll
-      for (int e = 0; e < 32; ++e) sa[e / 16][e % 16] = capped(sa[e / 16][e % 16]);
+      for (int e = 0; e < 32; ++e) sa[e / 16][e % 16] = capped(sa[e / 16][e % 16], rate);
     }
     top = largest(sa);
     int t = 0;
