@@ -358,7 +358,8 @@ int serq_g128_linear(const void* Xq, const float* scale, const int32_t* zero, in
  * Residual sum, root-mean-square norm, flattening and quantisation in one pass (Sec. 3.2, the decoder-layer flow of Fig. 2(b): the
  * flattening is merged into the norm before it):
  *   h[m,k]  = X[m,k] + residual[m,k], an fp32 sum rounded to x_dtype (no residual: h = X)
- *   rstd[m] = 1 / sqrt(mean_k h[m,k]^2 + eps), formed in 64 bits, rounded to fp32, at most the largest finite number (0 where the root is 0)
+ *   rstd[m] = 1 / sqrt(mean_k h[m,k]^2 + eps), formed in 64 bits, rounded to fp32, at most the largest finite number (0 where the root is 0 or
+ *           infinite)
  *   u[m,k]  = h[m,k] * gain[k], one fp32 multiply
  * gain [K] fp32 holds the norm's weight times the flattening factor s_inv, in permuted order; NULL: all ones.  The normalised row is
  * u rstd.  The integer codes are those of u on a grid of their own, to which rstd comes afterwards; with n bits,
@@ -372,6 +373,9 @@ int serq_g128_linear(const void* Xq, const float* scale, const int32_t* zero, in
  *   h_out [M,K] in x_dtype, row stride ldh: the sum, which the next layer's residual is.  It may be X or residual itself (same stride), but
  *         must not overlap them otherwise.
  *   eps   finite, not negative.
+ * A row whose sum holds an infinity (finite X and residual can add up to one) or NaN: h as it is, scale_out NaN, its codes and zero point undefined; MXFP4
+ * with an infinity: rstd = 0, so the other channels' codes are 0 (and their blocks' exponents 127), those of infinite channels undefined; with NaN: undefined.
+ * Other rows are not touched by it.
  * The sums of squares are exact enough for every output to be the same whatever the row's split (a sum of fp32 squares rounds in 64 bits).
  * M up to 2^30.  Everything else as the quantisers named.
  */

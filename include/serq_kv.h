@@ -77,7 +77,8 @@ int serq_kv_append(const void* q, int64_t ldq, int64_t ldqh, int q_heads,
 /*
  * The same for models that normalise the queries and keys of every head: before the rotation
  *   x[d] = fl(fl(x[d] * r) * weight[d]),   r = 1 / sqrt(mean_d x[d]^2 + eps) over the head's dim channels,
- * r formed in 64 bits, rounded to fp32, at most the largest finite number (0 where the root is 0).  q_weight for queries, k_weight for keys: [dim] fp32,
+ * r formed in 64 bits, rounded to fp32, at most the largest finite number (0 where the root is 0 or infinite: a head with an
+ * infinite channel becomes NaN there and 0 elsewhere before the rotation, one with NaN becomes NaN).  q_weight for queries, k_weight for keys: [dim] fp32,
  * 16-byte aligned, the same for all heads; NULL: those are not normalised (both NULL: serq_kv_append).  Values are never normalised.  eps finite, not
  * negative.  Everything else as serq_kv_append.
  */

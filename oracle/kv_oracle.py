@@ -19,12 +19,13 @@ def rotate(x, cos, sin, rot, interleaved, dtype=np.float64):
 
 def normed(x, weight, eps):
     """Every head of x [T, H, D] (fp32 values) by its root mean square: r = 1 / sqrt(mean x^2 + eps) formed in fp64 and rounded to fp32 (0 where the
-    root is 0), then two fp32 products."""
+    root is 0 or infinite), then two fp32 products."""
     x = np.asarray(x, np.float32)
     ms = (x.astype(np.float64) ** 2).sum(-1, keepdims=True) / x.shape[-1] + np.float64(np.float32(eps))
-    with np.errstate(divide="ignore", over="ignore"):
-        r = np.minimum(np.where(ms > 0, 1.0 / np.sqrt(ms), 0.0).astype(np.float32), np.finfo(np.float32).max)
-    return (x * r).astype(np.float32) * np.asarray(weight, np.float32)
+    with np.errstate(divide="ignore", over="ignore", invalid="ignore"):
+        r = np.minimum(np.where(ms == 0, 0.0, 1.0 / np.sqrt(ms)).astype(np.float32), np.finfo(np.float32).max)
+    with np.errstate(invalid="ignore"):
+        return (x * r).astype(np.float32) * np.asarray(weight, np.float32)
 
 
 def positions(cu, kv_len, T):

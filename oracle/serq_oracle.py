@@ -456,11 +456,11 @@ def mx_swiglu_quantize_act(gate, up, s_inv):
 
 def rmsnorm_rows(h: np.ndarray, gain, eps: float):
     """(u, rstd) of rows h (fp32 values of the stored sum): u = fl(h * gain), rstd = 1 / sqrt(mean h^2 + eps) formed in fp64, rounded to
-    fp32 and kept finite; 0 where the root is 0."""
+    fp32 and kept finite; 0 where the root is 0 or infinite."""
     h = np.asarray(h, F32)
     ms = (h.astype(np.float64) ** 2).sum(axis=1) / h.shape[1] + np.float64(F32(eps))
-    with np.errstate(divide="ignore", over="ignore"):
-        rstd = np.where(ms > 0, 1.0 / np.sqrt(ms), 0.0).astype(F32)
+    with np.errstate(divide="ignore", over="ignore", invalid="ignore"):
+        rstd = np.where(ms == 0, 0.0, 1.0 / np.sqrt(ms)).astype(F32)
     return flatten(h, gain), np.minimum(rstd, np.finfo(F32).max)
 
 

@@ -213,7 +213,8 @@ __global__ __launch_bounds__(KT) void rmsnorm_quantize_kernel(NormParams p) {
     if (m == p.M - 1 && (size_t)p.M < Mp)
       for (int blk = tid; blk < nblk8; blk += KT) xsc[((size_t)(blk >> 3) * Mp + (size_t)p.M) * 8 + (blk & 7)] = 127;
   } else if (tid == 0) {
-    ((float*)p.scale)[m] = unit > 0.0f ? sc * inv_root(ms) : 1.0f;
+    // (a sum that is not finite makes the token NaN, whatever the largest finite |u| is)
+    ((float*)p.scale)[m] = !(ms < __builtin_inf()) ? __builtin_nanf("") : unit > 0.0f ? sc * inv_root(ms) : 1.0f;
     if constexpr (ASYM) p.zero[m] = (int)z - (1 << (ABITS - 1));
   }
 }

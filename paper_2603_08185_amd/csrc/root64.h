@@ -33,9 +33,9 @@ __device__ __forceinline__ double wave_sum(double v) {
 }
 
 // 1 / sqrt(a) to within some 2^-50 (the instruction's own is good to about half of 64 bits' digits, a step of Newton's iteration doubles
-// them, the second is for its rounding), rounded to fp32 and kept finite; 0 for 0
+// them, the second is for its rounding), rounded to fp32 and kept finite; 0 for 0 and for infinity (whose first step would multiply infinity by 0), NaN for NaN
 __device__ __forceinline__ float inv_root(double a) {
-  if (!(a > 0.0)) return 0.0f;
+  if (!(a > 0.0 && a < __builtin_inf())) return a != a ? __builtin_nanf("") : 0.0f;
   double y = __builtin_amdgcn_rsq(a);
 #pragma unroll
   for (int i = 0; i < 2; ++i) y = __builtin_fma(0.5 * y, __builtin_fma(-a * y, y, 1.0), y);

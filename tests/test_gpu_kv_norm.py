@@ -177,3 +177,27 @@ def test_both_ways_from_python(monkeypatch):
         assert e.value.code == -4
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("D,rot", [(128, 128), (64, 32), (128, 0)])
+def test_heads_that_are_not_finite(fp8, inter, D, rot):
+    """An infinite channel: NaN there, zeros in the head's other channels, before the rotation; NaN: the whole head.  Other heads as ever."""
+    for dt in (torch.bfloat16, torch.float16):
+        B = Batch([(6, 9), (1, 3)], 4, 2, D, 16, dt, fp8, seed=9)
+        for x in (B.q, B.k):
+            x[0, 0, 5] = float("inf")
+            x[1, 1, D - 3] = -float("inf")
+            x[2, 0, 3] = float("nan")
+            x[3] = float("nan")
+            x[4, 1, 1], x[4, 1, 2] = float("inf"), float("nan")
+        cos, sin = _tables(20, rot) if rot else (None, None)
+        qw, kw = _weights(D, 3)
+        with np.errstate(invalid="ignore"):
+            want = _expected(B, cos, sin, inter, qw, kw, 1e-6)
+        assert want[0][0, 0].isnan().sum() == (2 if rot else 1) and (want[0][0, 0].nan_to_num() == 0).all() and want[0][2, 0].isnan().all()
+        q_out = serq.kv_append(B.q, B.k, B.v, *B.args(), cos, sin, interleaved=inter, k_scale=B.k_scale, v_scale=B.v_scale, q_norm=qw, k_norm=kw).cpu()
+        nan = want[0].isnan()
+        assert torch.equal(q_out.isnan(), nan) and torch.equal(_bits(q_out)[~nan], _bits(want[0])[~nan])
+        _same(B, torch.where(nan.to(DEV), want[0].to(DEV), q_out.to(DEV)), want, f"{dt}")

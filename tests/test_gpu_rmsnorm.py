@@ -239,3 +239,38 @@ def test_refuses_buffers_that_do_not_fit():
         serq.rmsnorm_quantize_act(x, gain, -1.0, 8, **ok)
     with pytest.raises(serq.SerqError):
         serq.rmsnorm_quantize_act(x, gain, 1e-6, 6, **ok)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("K", [64, 512, 4160, 33024])
+def test_rows_that_are_not_finite(form, K):
+    """Finite numbers whose sum overflows, infinities and NaN: they make their own token NaN (MXFP4: an infinite sum makes the other channels 0) and leave
+    the rows beside them alone."""
+    for dt in (torch.float16, torch.bfloat16, torch.float32):
+        x, r, gain = _inputs(7, K, dt, True, seed=K)
+        top, at = torch.finfo(dt).max, K // 2 + 1
+        x[1, at], r[1, at] = top, top                                  # finite terms
+        x[3, at] = -float("inf")
+        r[5, 0] = float("nan")
+        x[6] = float("nan")
+        bad, inf = [1, 3, 5, 6], [1, 3]
+        good = [0, 2, 4]
+        want = _want(x[good], r[good], gain, 1e-6, form)
+        h, Xq, sc, z = _call(x.to(DEV), r.to(DEV), gain.to(DEV), 1e-6, form)
+        ref = (x.float() + r.float()).to(dt)
+        assert torch.isinf(ref[1, at]) and torch.equal(h.cpu().nan_to_num(7.0), ref.nan_to_num(7.0)) and torch.equal(h.cpu().isnan(), ref.isnan())
+        assert torch.equal(_bits(h.cpu()[good]), _bits(want[0]))
+        if form == "mx":
+            codes, exps = (t.cpu().numpy() for t in serq.mx_unpack_act(Xq, sc, 7, K))
+            assert np.array_equal(codes[good], want[1]) and np.array_equal(exps[good], want[2])
+            others = np.arange(K) != at
+            assert (exps[inf] == 127).all() and not codes[inf][:, others].any(), "rstd is 0 there"
+            continue
+        codes = serq.unpack_act(Xq, int(form[-1]), 7, K).cpu().numpy()
+        assert np.array_equal(codes[good], want[1]) and np.array_equal(sc.cpu().numpy()[good], want[2])
+        assert torch.isnan(sc[bad]).all(), sc
+        if z is not None:
+            assert np.array_equal(z.cpu().numpy()[good], want[3])
+        none = torch.ones(K)
+        none[at] = 0                                                   # the infinite channel has no part in u
+        assert torch.isnan(_call(x.to(DEV), r.to(DEV), none.to(DEV), 1e-6, form)[2][bad]).all()
