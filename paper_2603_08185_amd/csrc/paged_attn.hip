@@ -140,7 +140,7 @@ size_t most_bytes(int64_t tokens, int seqs, int max_q, int64_t max_kv, int heads
   const int nb = rows > 16 ? 2 : 1;
   const int resident = nb > 1 ? paged_attn_few_resident(nb, false, D) : paged_attn_few_resident(nb, true, D);   // (the larger one: E4M3)
   size_t bytes = few_slots_bytes(few_shares(cus * resident, seqs, heads, max_kv), heads, nb, D);
-  if (D == 64 && heads % 2 == 0 && 2 * rows <= 16) {           // (two heads a time)
+  if (D == 64 && heads % 2 == 0 && 2 * group <= 16) {          // (two heads a time: a step of more rows has to serve those of fewer)
     const size_t pairs = few_slots_bytes(few_shares(cus * paged_attn_few_resident(1, false, 128), seqs, heads / 2, max_kv), heads / 2, 1, 128);
     if (pairs > bytes) bytes = pairs;
   }

@@ -41,3 +41,16 @@ def test_a_workspace_is_no_larger_than_what_can_be_used():
         few = 32768 + 2 * 512 * (16 if x[2] * 4 <= 16 else 32) * 130 * 4
         assert _size(*x) <= few + (0 if x[2] * 4 <= 32 else 46 << 20), x
     assert _size(1, 1, 1, 200) <= 32768 + 2 * 16 * 16 * 130 * 4    # (and a short sequence has few parts)
+
+
+@pytest.mark.parametrize("heads", [(16, 4, 64), (16, 16, 64), (4, 2, 64), (64, 8, 64), (6, 6, 64), (14, 2, 64), (3, 3, 64), (32, 8, 128)])
+def test_a_workspace_for_drafts_serves_single_tokens(heads):
+    """Steps of a few tokens, whose rows pass one kernel's limit after the other: none is smaller than a smaller step's."""
+    counts = [0, 1, 2, 3, 4, 5, 8, 9, 16, 17, 33]
+    for seqs in (1, 7, 8, 40):
+        for keys in (200, 4000, 32000, 65000, 131072):
+            sizes = [_size(max(seqs, q * seqs), seqs, q, keys, heads) for q in counts]
+            assert sizes == sorted(sizes), (seqs, keys, dict(zip(counts, sizes)))
+    for q in counts:
+        sizes = [_size(q, 1, q, keys, heads) for keys in (0, 1, 200, 4000, 16000, 32000, 65000, 131072, 1 << 20, 1 << 30)]
+        assert sizes == sorted(sizes), (q, sizes)
