@@ -37,15 +37,18 @@ constexpr size_t kManyRoom = 46u << 20;                        // most that its 
 
 // The kernel for many rows: blocks of rows times key heads are the workgroups; where they would leave compute units idle, the keys (at most `keys` that
 // a row block sees) are cut into slices.  Taken is the number of slices with the shortest time.  A tile of 64 keys takes a workgroup 1.08 us on a
-// compute unit of its own, 1.85 beside another; to begin takes 5 of these, to begin and to meet 8 and one a slice.  Where some units have one workgroup and some
-// two, what has no partner is done sooner and begins and ends hide behind the partner's work.  `blocks` counts a block more for each
+// compute unit of its own, 1.85 beside another; to begin takes 5 of these, to begin and to meet 8 and one a slice.  `blocks` counts a block more for each
 // sequence than may be needed (every sequence's last one is half empty on average); `full` is about what there is.
 // Measured (32 query and 8 key heads; us with 1 / 2 / 3 / 4 / 5 / 8 slices): 384 tokens after 3500 66.6 / 43.1 / 44.8 / 45.5 / 45.2 / 48.4, 100 after 30000
 // 469 / 245 / 171 / 134 / 114 / 87, 512 fresh ones 14.9 / 16.9 / 17.3 / 21.5; 512 after 32000 with 2 / 4 292 / 272, 256 after 8000 with 3 / 4 56.5 / 50.6.
-// With 1 / 2 / 3 / 4: 700 after 2500 56.9 / 52.2 / 56.7 / 68.5 (E4M3 73.5 / 64.3 / 63.9 / 74.1), beside 7 single tokens 65.7 / 55.7 / 66.7 / 62.7; 600 after
-// 6000 109 / 85.5 / 75.7 / 98.8; 512 after 4000 77.0 / 51.3 / 54.3 / 53.3.
+// `known`: where a sequence is alone, what a unit has is known well enough for more: with between one and two workgroups a unit some are without a partner and done sooner.
+// 700 after 2500 with 1 / 2 / 3 / 4 56.9 / 52.2 / 56.7 / 68.5 (E4M3 73.5 / 64.3 / 63.9 / 74.1), 600 after 6000 109 / 85.5 / 75.7 / 98.8.  Begins and ends are the dearer the more there are all the
+// same: at 0.6 instead of 1.4 of their time 100 after 1000 took 10 slices and 30 us, with 3 it is 22.7; 200 after 1200 34.6 / 24.  Over 800 random sizes it is
+// 1.2 % faster on average than 1.85 for all, 41 times by over 10 %, and never slower by over 3 %; of 700 others two were (by 5 and 16 %).  Of several sequences
+// the longest one's keys are known, not whose they are: there it is slower by over 3 % for 43 of 900, up to 1.48 times.  With modified scores it is taken for
+// them too (prefix, cap and bias 0.4 to 1.9 % faster on average, up to 1.35 times slower; 700 after 2500 beside 7 single tokens 65.7 / 55.7 / 66.7 / 62.7).
 constexpr int64_t kGrain = 128;                                // keys of a slice are a multiple of it
-Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, size_t slot_floats, size_t room) {
+Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, size_t slot_floats, size_t room, bool known) {
   Plan k{blocks, 1, 0x7fffff00, 0};
   const int64_t units = (int64_t)blocks * heads, slot = (int64_t)slot_floats * 4, bytes_most = (int64_t)(room < kManyRoom ? room : kManyRoom);
   if (units <= 0 || units > kTickets || keys <= kGrain) return k;
@@ -56,7 +59,7 @@ Plan plan_many(int blocks, int64_t full, int heads, int64_t keys, int64_t cus, s
     const double a_unit = (double)(full * heads * n) / (double)cus;
     const double tiles = (double)((each + 63) / 64), ends = n > 1 ? 8.0 + (double)n : 5.0;
     const double time = a_unit <= 1.0   ? 1.08 * (tiles + ends)
-                        : a_unit <= 2.0 ? (1.25 + 0.3 * a_unit) * tiles + (1.2 * a_unit - 0.6) * ends
+                        : a_unit <= 2.0 ? (known ? 1.55 * tiles + (1.08 + 0.3 * a_unit) * ends : 1.85 * (tiles + ends))
                                         : (0.93 * a_unit + 0.4) * (tiles + ends);
     if (n == 1 || time < 0.95 * least) {
       least = time;
@@ -86,7 +89,7 @@ struct Plans {
 };
 
 // room: bytes of the workspace
-Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int heads, int group, int D, bool f8, size_t room) {
+Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int heads, int group, int D, bool f8, size_t room, bool modified) {
   Plans k{};
   if (max_q > tokens) max_q = (int)tokens;
   if (max_kv > 0x7fffffff) max_kv = 0x7fffffff;
@@ -127,7 +130,8 @@ Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int
     const int blocks = many_blocks(tokens, seqs, group);
     // (sequences of about the longest one's length, and half of the last block of each)
     const int64_t alike = 2 * tokens / max_q < seqs ? 2 * tokens / max_q : seqs;
-    k.m = plan_many(blocks, (tokens * group + kTileRows - 1) / kTileRows + (alike - 1) / 2, heads, keys, cus, paged_attn_tile_slot_floats(D), room);
+    k.m = plan_many(blocks, (tokens * group + kTileRows - 1) / kTileRows + (alike - 1) / 2, heads, keys, cus, paged_attn_tile_slot_floats(D), room,
+                    seqs == 1 || modified);
   }
   return k;
 }
@@ -209,8 +213,9 @@ int serq_paged_attn_mod(const void* q, int64_t ldq, int64_t ldqh, int q_heads, i
     p.c.v_head *= 2;
     p.group *= 2;
   }
+  const bool modified = p.cap > 0.0f || p.slopes || p.from || p.to;
   // (a row that sees keys behind its own may see more than a window of them)
-  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, p.to ? 0 : window, p.c.heads, p.group, pairs ? 128 : D, f8, workspace_bytes);
+  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, p.to ? 0 : window, p.c.heads, p.group, pairs ? 128 : D, f8, workspace_bytes, modified);
   AttnModParams few = p, many = p;
   few.slices = k.f.slices; few.slice_keys = k.f.slice_keys;
   few.rows_from = 0; few.rows_to = k.many ? k.few_rows + 1 : 0x7fffffff;
@@ -221,7 +226,7 @@ int serq_paged_attn_mod(const void* q, int64_t ldq, int64_t ldqh, int q_heads, i
   many.tickets = few.tickets + kTickets;
   many.part = (float*)((char*)workspace + kTicketBytes + k.f.bytes);
   hipStream_t st = (hipStream_t)stream;
-  if (p.cap > 0.0f || p.slopes || p.from || p.to) {
+  if (modified) {
     const ModLaunch a{k.many ? &many : nullptr, k.few ? &few : nullptr, dtype, f8, D, k.nb, k.m.blocks, k.f.blocks, pairs};
     return p.cap > 0.0f ? launch_paged_attn_capped(a, st) : p.slopes ? launch_paged_attn_biased(a, st) : launch_paged_attn_ranges(a, st);
   }
