@@ -393,7 +393,8 @@ __device__ __forceinline__ void stretch(const ParamsOf<MOD>& p, const RowBlock& 
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[a][nb][e]);
       if (__ballot(top > ref[nb] + slack)) {
-        const float now = fmaxf(ref[nb], quads_reduce(top, [](float x, float y) { return fmaxf(x, y); }));
+        // (each row by its own keys: where a row's reference lies must not tell of what it does not see)
+        const float most = quads_reduce(top, [](float x, float y) { return fmaxf(x, y); }), now = most > ref[nb] + slack ? most : ref[nb];
         ref[nb] = now;
         const float mc = reference_of<MOD, DT>(now, c), f = exp2_fast(m[nb] - mc);
         m[nb] = mc;

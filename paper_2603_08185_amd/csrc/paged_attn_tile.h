@@ -297,7 +297,8 @@ __device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, char* lds_a
     if (__ballot(top > ref + slack)) {
       const uint32_t bits = __float_as_uint(top);
       const auto two = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
-      ref = fmaxf(ref, fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])));
+      const float most = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1]));
+      ref = most > ref + slack ? most : ref;                   // (by the row's own keys alone)
       const float mc = reference_of<MOD, DT>(ref, c), f = exp2_fast(m - mc);
       m = mc;
       sum *= f;

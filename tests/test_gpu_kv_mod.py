@@ -314,3 +314,23 @@ def test_one_workspace_for_all_kinds():
         plain = serq.paged_attention(B.q, *B.args(), B.max_q, B.max_kv, ws=ws)
         assert plain.shape == B.q.shape
         check_mod(B, *_run(B, ws))
+
+
+@pytest.mark.parametrize("mod", ["none", "cap", "bias", "docs"])
+@pytest.mark.parametrize("Hq,Hkv,D,dt", [(4, 2, 128, torch.bfloat16), (4, 4, 64, torch.float16), (2, 1, 64, torch.bfloat16)])
+def test_keys_of_other_rows_change_no_bit(mod, Hq, Hkv, D, dt):
+    """Large scores with keys that only the later rows of a block see: the earlier rows' weights are rounded as before, too."""
+    for n, L in ((4, 1200), (16, 300), (100, 700)):
+        kw = dict(MODS[mod]) if mod != "none" else {}
+        if mod == "docs":
+            kw = dict(ranges=lambda r, n, L: (np.zeros(n, int), np.where(np.arange(n) < n // 2, L - n, L)))
+        B = ModBatch([(n, L), (1, 50)], Hq, Hkv, D, 16, dt, seed=n, **kw)
+        want, lse = _run(B)
+        late, half = L - n + n // 2, n // 2                           # the first key that rows half, half + 1, ... see and those before do not
+        for factor in (30.0, -30.0, 0.0):
+            for j in range(late, L):
+                page = int(B.table[0, j // 16])
+                B.K[page, j % 16] *= factor
+            out, l2 = _run(B)
+            assert torch.equal(out[:half], want[:half]) and torch.equal(l2[:half], lse[:half]), (n, factor)
+            assert torch.equal(out[n:], want[n:]) and torch.equal(l2[n:], lse[n:])
