@@ -351,7 +351,10 @@ __device__ __forceinline__ bool last_to_arrive(uint32_t* ticket, int ns, int tid
 }
 size_t paged_attn_few_slot_floats(int nb, int D);
 int paged_attn_few_resident(int nb, bool f8, int D);          // workgroups that a compute unit runs together
-int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, bool pairs, int workgroups, hipStream_t st);
+int launch_paged_attn_few(const AttnParams& p, int dtype, bool f8, int D, int nb, int workgroups, hipStream_t st);
+// heads of 64 channels one a time, or two where the line has `long_line` pieces: workgroups of either, and slice_keys of two
+struct PairPlan { int one, two, long_line, two_keys; };
+int launch_paged_attn_pairs(const AttnParams& p, int dtype, const PairPlan& n, hipStream_t st);
 size_t paged_attn_tile_slot_floats(int D);
 int launch_paged_attn_tile(const AttnParams& p, int dtype, bool f8, int D, int blocks, hipStream_t st);
 int launch_paged_attn_mixed(const AttnParams& many, const AttnParams& few, int dtype, bool f8, int D, int blocks, int shares, hipStream_t st);
@@ -359,7 +362,7 @@ int launch_paged_attn_mixed(const AttnParams& many, const AttnParams& few, int d
 struct ModLaunch {
   const AttnModParams* many; const AttnModParams* few;        // null: none
   int dtype; bool f8; int D, nb, blocks, shares;              // blocks: of the kernel for many rows, shares: workgroups of the one for few
-  bool pairs;                                                 // two key heads of 64 channels a time (few rows alone)
+  PairPlan pairs;                                             // few rows alone: two key heads of 64 channels a time (`two` is 0: no)
 };
 int launch_paged_attn_ranges(const ModLaunch& a, hipStream_t st);
 int launch_paged_attn_capped(const ModLaunch& a, hipStream_t st);

@@ -88,11 +88,19 @@ struct Plans {
   Plan f, m;
 };
 
+// keys that a row sees at most
+int64_t seen_keys(int64_t max_kv, int window, int max_q) {
+  if (max_kv > 0x7fffffff) max_kv = 0x7fffffff;
+  return window > 0 && max_kv > (int64_t)window + max_q ? (int64_t)window + max_q : max_kv;
+}
+
+// Keys times key heads of all sequences from which on narrow heads go two a time (few::work_pairs has the measurements), by the rows of two heads.
+int64_t pairs_from(int64_t rows) { return (rows > 6 ? rows : 6) << 17; }
+
 // room: bytes of the workspace
 Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int heads, int group, int D, bool f8, size_t room, bool modified) {
   Plans k{};
   if (max_q > tokens) max_q = (int)tokens;
-  if (max_kv > 0x7fffffff) max_kv = 0x7fffffff;
   const int64_t rows = (int64_t)max_q * group;
   // The kernel for few rows holds 16 or 32 of them.  Measured on sequences of 17 to 32 (us, few rows / many; 4 rows a token): 1 of 8 tokens after 4000
   // 25.1 / 27.9, 1 of 6 after 30000 56.3 / 68.1, 1 of 5 after 300 13.1 / 10.2, 4 of 5 after 3000 29.3 / 26.1: it holds its own where keys are many, and
@@ -102,9 +110,7 @@ Plans plans(int64_t tokens, int seqs, int max_q, int64_t max_kv, int window, int
   // beside a chunk, what is short is a token or a few
   k.few_rows = k.many && group <= 16 ? 16 : 32;
   k.nb = rows <= 16 || k.few_rows == 16 ? 1 : 2;
-  int64_t keys = max_kv;
-  if (window > 0 && keys > (int64_t)window + max_q) keys = (int64_t)window + max_q;
-  const int64_t cus = device_cu_count();
+  const int64_t keys = seen_keys(max_kv, window, max_q), cus = device_cu_count();
   room = room > kTicketBytes ? room - kTicketBytes : 0;
   if (k.few) {
     // As many workgroups as run together, each with an equal share of a head's keys; or a workgroup for every sequence and head, where sequences are
@@ -144,7 +150,8 @@ size_t most_bytes(int64_t tokens, int seqs, int max_q, int64_t max_kv, int heads
   const int nb = rows > 16 ? 2 : 1;
   const int resident = nb > 1 ? paged_attn_few_resident(nb, false, D) : paged_attn_few_resident(nb, true, D);   // (the larger one: E4M3)
   size_t bytes = few_slots_bytes(few_shares(cus * resident, seqs, heads, max_kv), heads, nb, D);
-  if (D == 64 && heads % 2 == 0 && 2 * group <= 16) {          // (two heads a time: a step of more rows has to serve those of fewer)
+  // (two heads a time: by the least rows, since a step of more of them has to serve those of fewer)
+  if (D == 64 && heads % 2 == 0 && 2 * group <= 16 && seqs * max_kv * heads >= pairs_from(2 * group)) {
     const size_t pairs = few_slots_bytes(few_shares(cus * paged_attn_few_resident(1, false, 128), seqs, heads / 2, max_kv), heads / 2, 1, 128);
     if (pairs > bytes) bytes = pairs;
   }
@@ -203,19 +210,9 @@ int serq_paged_attn_mod(const void* q, int64_t ldq, int64_t ldqh, int q_heads, i
   // (as wide as the table or wider: it hides nothing, and the position of a token before the start less such a window would not fit 32 bits)
   if (window >= (int64_t)batch->table_width * cache->page_size) p.window = window = 0;
   if (!workspace) workspace_bytes = 0;
-  // narrow heads side by side in memory: two a time, where both heads' rows fit the kernel for few
-  int64_t rows = max_q < batch->tokens ? max_q : batch->tokens;
-  rows *= p.group;
-  const bool pairs = !f8 && D == 64 && cache->heads % 2 == 0 && cache->k_head == 64 && cache->v_head == 64 && 2 * rows <= 16;
-  if (pairs) {
-    p.c.heads /= 2;
-    p.c.k_head *= 2;
-    p.c.v_head *= 2;
-    p.group *= 2;
-  }
   const bool modified = p.cap > 0.0f || p.slopes || p.from || p.to;
-  // (a row that sees keys behind its own may see more than a window of them)
-  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, p.to ? 0 : window, p.c.heads, p.group, pairs ? 128 : D, f8, workspace_bytes, modified);
+  if (p.to) window = 0;                                       // (a row that sees keys behind its own may see more than a window of them)
+  const Plans k = plans(batch->tokens, batch->seqs, max_q, max_kv, window, p.c.heads, p.group, D, f8, workspace_bytes, modified);
   AttnModParams few = p, many = p;
   few.slices = k.f.slices; few.slice_keys = k.f.slice_keys;
   few.rows_from = 0; few.rows_to = k.many ? k.few_rows + 1 : 0x7fffffff;
@@ -226,13 +223,22 @@ int serq_paged_attn_mod(const void* q, int64_t ldq, int64_t ldqh, int q_heads, i
   many.tickets = few.tickets + kTickets;
   many.part = (float*)((char*)workspace + kTicketBytes + k.f.bytes);
   hipStream_t st = (hipStream_t)stream;
+  // narrow heads side by side in memory: two a time, where both heads' rows fit the kernel for few and the line may be long enough
+  PairPlan pairs{};
+  const int64_t rows = 2 * (int64_t)p.group * (max_q < 1 ? 1 : max_q < batch->tokens ? max_q : batch->tokens), from = pairs_from(rows);
+  if (!f8 && D == 64 && p.c.heads % 2 == 0 && cache->k_head == 64 && cache->v_head == 64 && rows <= 16 && k.f.slices > 1 &&
+      batch->seqs * seen_keys(max_kv, window, max_q) * p.c.heads >= from) {
+    const Plans t = plans(batch->tokens, batch->seqs, max_q, max_kv, window, p.c.heads / 2, 2 * p.group, 128, f8, workspace_bytes, modified);
+    if (t.f.slices > 1) pairs = PairPlan{k.f.blocks, t.f.blocks, (int)((from + 64 * p.c.heads - 1) / (64 * p.c.heads)), t.f.slice_keys};
+  }
   if (modified) {
     const ModLaunch a{k.many ? &many : nullptr, k.few ? &few : nullptr, dtype, f8, D, k.nb, k.m.blocks, k.f.blocks, pairs};
     return p.cap > 0.0f ? launch_paged_attn_capped(a, st) : p.slopes ? launch_paged_attn_biased(a, st) : launch_paged_attn_ranges(a, st);
   }
+  if (pairs.two) return launch_paged_attn_pairs(few, dtype, pairs, st);
   if (k.few && k.many && k.nb == 1) return launch_paged_attn_mixed(many, few, dtype, f8, D, k.m.blocks, k.f.blocks, st);
   if (k.many && (rc = launch_paged_attn_tile(many, dtype, f8, D, k.m.blocks, st)) != SERQ_OK) return rc;
-  return k.few ? launch_paged_attn_few(few, dtype, f8, D, k.nb, pairs, k.f.blocks, st) : SERQ_OK;
+  return k.few ? launch_paged_attn_few(few, dtype, f8, D, k.nb, k.f.blocks, st) : SERQ_OK;
 }
 
 int serq_paged_attn(const void* q, int64_t ldq, int64_t ldqh, int q_heads, int dtype, const serq_kv_cache* cache,

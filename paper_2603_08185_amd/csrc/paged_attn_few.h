@@ -493,39 +493,30 @@ __device__ __forceinline__ void stretch(const ParamsOf<MOD>& p, const RowBlock& 
 
 constexpr int kUnit = 64;                                     // keys of a piece of a line
 
-// What workgroup `id` of `count` does.  lds: kLds bytes, 16-byte aligned.
-template <bool F8, int D, int NB> constexpr int kLds = kWaves * Few<F8, D, NB>::REGION;
-template <int DT, bool F8, int D, int NB, int MOD = kPlain, bool PAIRS = false>
-__device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, int count, char* lds) {
-  constexpr int BM = 16 * NB;
-  __shared__ float stat[kWaves][BM][2];
-  const int heads = p.c.heads;
-  // neighbouring workgroups have different key heads
-  const int number = uniform(id / heads), h = id - number * heads;
-  if (p.slices <= 1) {                                        // nowhere to meet: a workgroup takes a sequence whole
-    const int c0 = uniform(p.c.cu[number]), n = uniform(p.c.cu[number + 1]) - c0;
-    if (!takes(p, c0, n)) return;
-    const RowBlock k = block_of<BM>(p, number, c0, n, uniform(p.c.len[number]), 0);
-    stretch<DT, F8, D, NB, MOD, PAIRS>(p, k, h, k.begin & ~15, max(k.end, 0), false, {}, lds, stat);
-    return;
-  }
-  // (a sequence has one piece at least: its rows have to be written)
-  const auto pieces = [&](int c0, int n, int L) {
-    if constexpr (MOD != kPlain) {                            // (what block_of finds for the same rows)
-      if (kLookAlways<BM> || p.from || p.to) {
-        const int tokens = (min(n * p.group, BM) + p.group - 1) / p.group;
-        Seen s;
-        for (int i = 0; i < tokens; ++i) s.add(row_range(p, c0 + i, L - n + i, L));
-        const int base = s.begin & ~15;
-        return s.end > 0 ? (s.end - base - 1) / kUnit + 1 : 1;
-      }
+// The pieces that a sequence gives a key head's line (one at least: its rows have to be written).
+template <int NB, int MOD>
+__device__ __forceinline__ int pieces_of(const ParamsOf<MOD>& p, int c0, int n, int L) {
+  if constexpr (MOD != kPlain) {                              // (what block_of finds for the same rows)
+    constexpr int BM = 16 * NB;
+    if (kLookAlways<BM> || p.from || p.to) {
+      const int tokens = (min(n * p.group, BM) + p.group - 1) / p.group;
+      Seen s;
+      for (int i = 0; i < tokens; ++i) s.add(row_range(p, c0 + i, L - n + i, L));
+      const int base = s.begin & ~15;
+      return s.end > 0 ? (s.end - base - 1) / kUnit + 1 : 1;
     }
-    const int end = min(L, p.c.width << p.c.page_shift), base = (p.window > 0 ? max(0, L - n - p.window + 1) : 0) & ~15;
-    return end > base ? (end - base - 1) / kUnit + 1 : 1;
-  };
-  Line line(p, pieces, threadIdx.x & 63);
+  }
+  const int end = min(L, p.c.width << p.c.page_shift), base = (p.window > 0 ? max(0, L - n - p.window + 1) : 0) & ~15;
+  return end > base ? (end - base - 1) / kUnit + 1 : 1;
+}
+
+// Share `number` of the `wanted` that key head h's line is cut into.  lds: kLds bytes, 16-byte aligned.
+template <bool F8, int D, int NB> constexpr int kLds = kWaves * Few<F8, D, NB>::REGION;
+template <int DT, bool F8, int D, int NB, int MOD, bool PAIRS, class L>
+__device__ __forceinline__ void walk(const ParamsOf<MOD>& p, L& line, int number, int wanted, int h, char* lds, float (*stat)[16 * NB][2]) {
+  constexpr int BM = 16 * NB;
   // a share: of the head's line, but not too little for a workgroup, nor so little that too many meet
-  const int wanted = count / heads, total = line.total;
+  const int total = line.total;
   const int share = max(max(p.slice_keys / kUnit, total / (kMaxSlices - 2) + 1), (total + wanted - 1) / wanted);
   int at = (int)min((int64_t)number * share, (int64_t)total);
   const int stop = min(at + share, total);
@@ -545,6 +536,55 @@ __device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, int count, 
     at = until;
     __syncthreads();                                          // LDS is free again
   }
+}
+
+// What workgroup `id` of `count` does.  lds: kLds bytes, 16-byte aligned.
+template <int DT, bool F8, int D, int NB, int MOD = kPlain>
+__device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, int count, char* lds) {
+  constexpr int BM = 16 * NB;
+  __shared__ float stat[kWaves][BM][2];
+  const int heads = p.c.heads;
+  // neighbouring workgroups have different key heads
+  const int number = uniform(id / heads), h = id - number * heads;
+  if (p.slices <= 1) {                                        // nowhere to meet: a workgroup takes a sequence whole
+    const int c0 = uniform(p.c.cu[number]), n = uniform(p.c.cu[number + 1]) - c0;
+    if (!takes(p, c0, n)) return;
+    const RowBlock k = block_of<BM>(p, number, c0, n, uniform(p.c.len[number]), 0);
+    stretch<DT, F8, D, NB, MOD, false>(p, k, h, k.begin & ~15, max(k.end, 0), false, {}, lds, stat);
+    return;
+  }
+  const auto pieces = [&](int c0, int n, int L) { return pieces_of<NB, MOD>(p, c0, n, L); };
+  Line line(p, pieces, threadIdx.x & 63);
+  walk<DT, F8, D, NB, MOD, false>(p, line, number, count / heads, h, lds, stat);
+}
+
+// Heads of 64 channels side by side in memory, one a time or two (PAIRS).  Two a time read 256 bytes in a row, but a share of two heads' keys is twice the work and
+// slots of twice the rows and twice the channels are joined, which pays once the line is long: from `long_line` pieces on.  How long it is is known here alone
+// (the host has bounds, and a captured graph has them for every step to come).  Measured (us, one a time / two; one token a sequence of alike
+// lengths, key heads x rows of each):
+//   16 x 1   one over 1000 keys 8.3 / 10.7, over 16000 22.1 / 19.9, over 65000 62.9 / 53.1;  40 over 1600 66.4 / 58.4
+//    8 x 4   one over 1000 8.3 / 10.4, over 16000 15.3 / 20.3;  4 over 8000 24.1 / 22.9, over 32000 63.8 / 54.8;  40 over 6500 122 / 107
+//    2 x 7   one over 65000 19.7 / 39.5;  12 over 22000 34.1 / 38.5, over 87000 97.0 / 95.6
+//    4 x 1   4 over 16000 21.2 / 24.8, over 33000 32.4 / 34.5, over 65000 56.2 / 55.4
+// Of 536 sizes, bounds far above the lengths and lengths far apart among them, none is slower than with one a time alone by over 3 %, 103 are faster.
+template <int DT, int MOD>
+__device__ __forceinline__ void work_pairs(const ParamsOf<MOD>& p, const PairPlan& n, int id, char* lds) {
+  __shared__ float stat[kWaves][16][2];
+  const int heads = p.c.heads, number = uniform(id / heads), h = id - number * heads, wanted = n.one / heads;
+  const auto pieces = [&](int c0, int m, int L) { return pieces_of<1, MOD>(p, c0, m, L); };
+  Line line(p, pieces, threadIdx.x & 63);
+  if (line.total < n.long_line) {
+    if (number < wanted) walk<DT, false, 64, 1, MOD, false>(p, line, number, wanted, h, lds, stat);
+    return;
+  }
+  ParamsOf<MOD> two = p;
+  two.c.heads /= 2;
+  two.c.k_head *= 2;
+  two.c.v_head *= 2;
+  two.group *= 2;
+  two.slice_keys = n.two_keys;
+  const int number2 = uniform(id / two.c.heads);
+  if (id < n.two) walk<DT, false, 128, 1, MOD, true>(two, line, number2, n.two / two.c.heads, id - number2 * two.c.heads, lds, stat);
 }
 
 }  // namespace few

@@ -35,9 +35,9 @@ __global__ __launch_bounds__(256, 2) void paged_attn_mod_mixed_kernel(AttnModPar
 }
 
 template <int DT, int MOD>
-__global__ __launch_bounds__(256, 2) void paged_attn_mod_few_pairs_kernel(AttnModParams p) {
+__global__ __launch_bounds__(256, 2) void paged_attn_mod_few_pairs_kernel(AttnModParams p, PairPlan n) {
   __shared__ __align__(16) char lds[few::kLds<false, 128, 1>];
-  few::work<DT, false, 128, 1, MOD, true>(p, blockIdx.x, gridDim.x, lds);
+  few::work_pairs<DT, MOD>(p, n, blockIdx.x, lds);
 }
 
 template <int MOD, int DT, bool F8, int D>
@@ -56,9 +56,10 @@ int launch_mod_of(const ModLaunch& a, hipStream_t st) {
 template <int MOD>
 int launch_mod(const ModLaunch& a, hipStream_t st) {
   const bool bf = a.dtype == SERQ_BF16;
-  if (a.pairs) {
-    if (bf) hipLaunchKernelGGL((paged_attn_mod_few_pairs_kernel<SERQ_BF16, MOD>), dim3((unsigned)a.shares), dim3(256), 0, st, *a.few);
-    else hipLaunchKernelGGL((paged_attn_mod_few_pairs_kernel<SERQ_F16, MOD>), dim3((unsigned)a.shares), dim3(256), 0, st, *a.few);
+  if (a.pairs.two) {
+    const dim3 grid((unsigned)(a.pairs.one > a.pairs.two ? a.pairs.one : a.pairs.two));
+    if (bf) hipLaunchKernelGGL((paged_attn_mod_few_pairs_kernel<SERQ_BF16, MOD>), grid, dim3(256), 0, st, *a.few, a.pairs);
+    else hipLaunchKernelGGL((paged_attn_mod_few_pairs_kernel<SERQ_F16, MOD>), grid, dim3(256), 0, st, *a.few, a.pairs);
     return hipGetLastError() == hipSuccess ? SERQ_OK : SERQ_EHIP;
   }
   if (a.D == 128) {
