@@ -252,23 +252,36 @@ __device__ __forceinline__ void work(const ParamsOf<MOD>& p, int id, char* lds_a
     const int key0 = k0 + t * kKeys;
     if (key0 < k.begin || key0 + kKeys > k.end || key0 < k.all_from || key0 + kKeys > k.all_to) {
       // values of keys that no row sees become zero (a weight of zero does not make NaN zero); of those that some see, what is not finite
-      // (that test eight values a time, since most often all are: 12000 tokens of packed documents 180 us without it, 158 with it)
-      constexpr int N = F8 ? 1 : TILE / 16 / (64 * NW);        // pieces a time (E4M3: registers; capped prompt of 8192 tokens 657 / 636 us)
+      if constexpr (F8 && MOD == kPlain) {
+        // (straight on: the other way spills 4 registers more and has few such tiles to make up for it: 384 after 3500 beside 8 single tokens 54.6 / 55.4 us,
+        // 512 fresh ones 18.5 / 19.0, a prompt of 8192 551 / 555)
+        bool found = false;
+        for (int at = tid; at < TILE / 16; at += 64 * NW) {
+          const int key = key0 + at / (ROW / 16);
+          u4* v = (u4*)(lds[t & 1][1] + at * 16);
+          if (key < k.begin || key >= k.end) *v = (u4){0, 0, 0, 0};
+          else if (key < k.all_from || key >= k.all_to) *v = take_out<DT>(*v, found);
+        }
+        if (found) odd = 1;
+      } else {
+        // (tested eight values a time, since most often all are: 12000 tokens of packed documents 180 us without it, 158 with it; E4M3 186 / 179)
+        constexpr int N = F8 ? 1 : TILE / 16 / (64 * NW);      // pieces a time (E4M3: registers; capped prompt of 8192 tokens 657 / 636 us)
 #pragma unroll 1
-      for (int at = tid; at < TILE / 16; at += 64 * NW * N) {
-        u4* const v = (u4*)(lds[t & 1][1]) + at;
-        u4 x[N];
+        for (int at = tid; at < TILE / 16; at += 64 * NW * N) {
+          u4* const v = (u4*)(lds[t & 1][1]) + at;
+          u4 x[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = v[64 * NW * i];
+          for (int i = 0; i < N; ++i) x[i] = v[64 * NW * i];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int key = key0 + (at + 64 * NW * i) / (ROW / 16);
-          if (key < k.begin || key >= k.end) {
-            v[64 * NW * i] = (u4){0, 0, 0, 0};
-          } else if ((key < k.all_from || key >= k.all_to) && any_odd<DT>(x[i])) {
-            bool found = false;
-            v[64 * NW * i] = take_out<DT>(x[i], found);
-            odd = 1;
+          for (int i = 0; i < N; ++i) {
+            const int key = key0 + (at + 64 * NW * i) / (ROW / 16);
+            if (key < k.begin || key >= k.end) {
+              v[64 * NW * i] = (u4){0, 0, 0, 0};
+            } else if ((key < k.all_from || key >= k.all_to) && any_odd<DT>(x[i])) {
+              bool found = false;
+              v[64 * NW * i] = take_out<DT>(x[i], found);
+              odd = 1;
+            }
           }
         }
       }
