@@ -892,6 +892,8 @@ def paged_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table: to
         raise ValueError("lse must be fp32 [tokens, q_heads] in device memory")
     if ws is not None and (not ws.is_cuda or ws.dtype != torch.uint8 or not ws.is_contiguous()):
         raise ValueError("ws must be a uint8 buffer in device memory")
+    if cap != 0 and C.c_float(cap).value == 0:
+        raise ValueError("cap must be a positive fp32 number, or 0 for none")
     for t, what, dt, n in ((slopes, "slopes", torch.float32, q.shape[1]), (see_from, "see_from", torch.int32, q.shape[0]),
                            (see_to, "see_to", torch.int32, q.shape[0])):
         if t is not None and (not t.is_cuda or t.dtype != dt or t.shape != (n,) or not t.is_contiguous()):

@@ -473,6 +473,7 @@ PyObject* paged_attention_mod(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Attention r = attention(x);
     serq_attn_mod m{};
     m.cap = x.real(15);
+    if (x.ok && m.cap == 0.0f && PyFloat_AS_DOUBLE(x.a[15]) != 0.0) x.ok = false;   // (too small for fp32: not "no cap")
     m.slopes = scales(x, 16, r.q.H);
     const int32_t** const see[2] = {&m.see_from, &m.see_to};
     for (int i = 0; i < 2; ++i) {

@@ -334,3 +334,20 @@ def test_keys_of_other_rows_change_no_bit(mod, Hq, Hkv, D, dt):
             out, l2 = _run(B)
             assert torch.equal(out[:half], want[:half]) and torch.equal(l2[:half], lse[:half]), (n, factor)
             assert torch.equal(out[n:], want[n:]) and torch.equal(l2[n:], lse[n:])
+
+
+def test_caps_too_small_for_fp32(monkeypatch):
+    """A cap that is 0 in fp32 is refused, not taken for none; 0 of either sign or type is none."""
+    B = ModBatch(SETS["few"], 4, 2, 64, 16, seed=3)
+    fast = serq._fast
+    for mod in (fast, _General()):
+        monkeypatch.setattr(serq, "_fast", mod)
+        for cap in (1e-50, -1e-50, 5e-324, 2.0 ** -151):
+            for more in ({}, dict(slopes=torch.ones(4, device=DEV)), dict(see_from=torch.zeros(B.T, dtype=torch.int32, device=DEV))):
+                with pytest.raises(ValueError):
+                    _run(B, cap=cap, **more)
+        want = _run(B, cap=0.0)
+        for cap in (0, -0.0):
+            for a, b in zip(_run(B, cap=cap), want):
+                assert torch.equal(a, b)
+        _run(B, cap=2.0 ** -149)
