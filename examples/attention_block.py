@@ -5,8 +5,8 @@
 Every step runs what a server runs for a layer: quantise the residual stream, the fused q/k/v projection, rotate and append to the paged
 cache, attention over it, quantise, the o projection.  Sequences of different lengths share the cache's pages; the prompts go through in
 one ragged call, the tokens after them one a sequence, recorded into a graph once and replayed (lengths live in device memory).
-With --norms the stream is a model's: what the block gives is added to it and the sum normalised in the pass that quantises it, and the heads of q and k
-are normalised before they are rotated.  --cap caps the scores.  Weights are random: the numbers show the path, not a language.
+With --norms the stream is a model's: what the block gives is the next step's x, which is added to the stream and the sum normalised in the pass that
+quantises it, and the heads of q and k are normalised before they are rotated.  --cap caps the scores.  Weights are random: the numbers show the path, not a language.
 """
 from __future__ import annotations
 
@@ -91,12 +91,18 @@ def run(block, prompts, steps, seed=1):
     x, one, kv_len, b = new(B), i32(list(range(B + 1))), i32(prompts), block.buffers(B, B, 1, most)
     stream = torch.zeros_like(x) if block.norms else None
     kv_len += 1
-    block.step(x, table, one, kv_len, b, stream)                  # warm, and the token that the graph's first replay follows
+    def token():
+        y = block.step(x, table, one, kv_len, b, stream)
+        if block.norms:
+            x.copy_(y)
+        return y
+
+    token()                                                       # warm, and the token that the graph's first replay follows
     graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
     torch.cuda.synchronize()
     with torch.cuda.graph(graph, stream=side):
         kv_len += 1
-        y = block.step(x, table, one, kv_len, b, stream)
+        y = token()
     torch.cuda.synchronize()
     began = time.perf_counter()
     for _ in range(steps):

@@ -65,3 +65,30 @@ def test_a_block_with_norms(fp8, cap, monkeypatch):
                 want, _, mag, eo, _ = kvo.attention_mod(q[rows].double().cpu().numpy(), kk, vv, 64 ** -0.5, L - n, np.zeros(n), at + 1, cap)
                 tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -7 + 2.0 ** -15) * mag + 2 * eo
                 assert (np.abs(out[0][rows].double().cpu().numpy() - want) <= tol).all(), b
+
+
+def test_what_the_block_gives_goes_back_into_the_stream():
+    """The example's graph against the same steps one by one: each step's output is the next one's x, which is added to the stream."""
+    ex = _example()
+    blocks = [ex.AttentionBlock(hidden=512, q_heads=8, kv_heads=2, dim=64, rank=32, pages=64, page=16, norms=True, cap=6.0) for _ in range(2)]
+    prompts, steps = [70, 3, 130], 4
+    first, y, kv_len, table, _ = ex.run(blocks[0], prompts, steps)
+    block, g = blocks[1], torch.Generator(device=DEV).manual_seed(1)
+    torch.randperm(block.K.shape[0], generator=g, device=DEV)
+    new = lambda n: torch.randn((n, block.hidden), generator=g, device=DEV).to(block.dtype)
+    cu = torch.tensor([0, 70, 73, 203], dtype=torch.int32, device=DEV)
+    lens = torch.tensor(prompts, dtype=torch.int32, device=DEV)
+    x, most = new(203), max(prompts) + steps + 1
+    out = block.step(x, table, cu, lens, block.buffers(203, 3, 130, 130), torch.zeros_like(x))
+    assert torch.equal(out, first)
+    x, one, b = new(3), torch.arange(4, dtype=torch.int32, device=DEV), block.buffers(3, 3, 1, most)
+    stream = torch.zeros_like(x)
+    for _ in range(steps + 1):
+        lens += 1
+        before = stream.clone()
+        out = block.step(x, table, one, lens, b, stream).clone()
+        assert torch.equal(stream, (x.float() + before.float()).to(x.dtype))
+        x = out
+    assert torch.equal(lens, kv_len) and torch.equal(out, y)
+    for a, c in ((blocks[0].K, block.K), (blocks[0].V, block.V)):
+        assert torch.equal(a, c)
