@@ -92,3 +92,37 @@ def test_what_the_block_gives_goes_back_into_the_stream():
     assert torch.equal(lens, kv_len) and torch.equal(out, y)
     for a, c in ((blocks[0].K, block.K), (blocks[0].V, block.V)):
         assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_what_the_append_writes(fp8, monkeypatch):
+    """Keys and values of a block's steps as they lie in the cache: normalised and rotated keys, values as they are, each in its own slot, bit for bit, and
+    every other slot as it was."""
+    ex = _example()
+    block = ex.AttentionBlock(hidden=512, q_heads=8, kv_heads=2, dim=64, rank=32, pages=64, page=16, fp8=fp8, norms=True)
+    for cache in (block.K, block.V):
+        cache.view(torch.uint8).random_(0, 120, generator=torch.Generator(device=DEV).manual_seed(2))
+    seen, real = [], serq.kv_append
+
+    def spy(q, k, v, K, V, *a, **kw):
+        if len(seen) == 2:                                        # the prompts' step, the first token's; then the graph's
+            return real(q, k, v, K, V, *a, **kw)
+        before = [t.clone() for t in (q, k, v, K, V, a[1], a[2])]
+        out = real(q, k, v, K, V, *a, **kw)
+        seen.append((before, a, kw, K.clone(), V.clone()))
+        return out
+
+    monkeypatch.setattr(serq, "kv_append", spy)
+    ex.run(block, [70, 3, 130], 2)
+    bits = lambda t: t.contiguous().view(torch.uint8).cpu()
+    for (q, k, v, K, V, cu, ln), (table, _, _, cos, sin), kw, K1, V1 in seen:
+        seq, pos = kvo.positions(cu.cpu().numpy(), ln.cpu().numpy(), k.shape[0])
+        page, row = (torch.from_numpy(np.asarray(x)).to(DEV) for x in kvo.slots(seq, pos, table.cpu().numpy(), 16, 64))
+        assert (page >= 0).all() and len(set(zip(page.tolist(), row.tolist()))) == k.shape[0]
+        keys = kvo.rotate(kvo.normed(f32(k), f32(kw["k_norm"]), 1e-6), f32(cos)[pos], f32(sin)[pos], 64, False, np.float32)
+        for cache, after, x, s in ((K, K1, keys, kw["k_scale"]), (V, V1, f32(v), kw["v_scale"])):
+            want = cache.clone()
+            x = torch.from_numpy(x).to(DEV)
+            x = (x / s[:, None]).clamp(-448, 448) if fp8 else x
+            want.view(torch.uint8)[page, row] = x.to(cache.dtype).view(torch.uint8)
+            assert torch.equal(bits(after), bits(want))

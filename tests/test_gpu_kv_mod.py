@@ -351,3 +351,25 @@ def test_caps_too_small_for_fp32(monkeypatch):
             for a, b in zip(_run(B, cap=cap), want):
                 assert torch.equal(a, b)
         _run(B, cap=2.0 ** -149)
+
+
+def test_plain_calls_between_modified_ones():
+    """Plain calls on a workspace that modified ones leave behind, and the other way round: each as on a workspace of its own, bit by bit."""
+    Bs = [ModBatch(SETS[n], 4, 2, 64, 16, seed=i, **MODS[m]) for i, (n, m) in enumerate((("long", "cap"), ("ones", "bias"), ("chunk", "docs"), ("few", "wild"), ("ones", "cap")))]
+    most = [max(f(B) for B in Bs) for f in (lambda B: B.T, lambda B: len(B.seqs), lambda B: B.max_q, lambda B: B.max_kv)]
+    room = lambda: serq.paged_attention_workspace(*most, 4, 2, 64, DEV)
+
+    def plain(B, ws):
+        lse = torch.empty((B.T, 4), device=DEV)
+        table = torch.where((B.d_table < 0) | (B.d_table >= B.pages), 0, B.d_table)    # (a plain row sees pages that the modified ones do not)
+        return serq.paged_attention(B.q, B.K, B.V, table, B.d_cu, B.d_len, B.max_q, B.max_kv, lse=lse, ws=ws), lse
+
+    for B in Bs:
+        for t in (B.K, B.V):
+            t.nan_to_num_(nan=0.25)
+    alone = [(plain(B, room()), _run(B, room())) for B in Bs]
+    assert all(torch.isfinite(x.float()).all() for (a, _) in alone for x in a)
+    ws = room()
+    for i in (0, 1, 2, 3, 4, 4, 3, 2, 1, 0):
+        for got, want in zip((plain(Bs[i], ws), _run(Bs[i], ws)), alone[i]):
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), i
