@@ -274,3 +274,11 @@ def test_rows_that_are_not_finite(form, K):
         none = torch.ones(K)
         none[at] = 0                                                   # the infinite channel has no part in u
         assert torch.isnan(_call(x.to(DEV), r.to(DEV), none.to(DEV), 1e-6, form)[2][bad]).all()
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("K", [2048, 2112, 2624, 3008, 3136, 4032, 4096, 4160])
+def test_many_rows_without_a_residual(form, K):
+    """More than 1000 rows and nothing to add: other threads a row there."""
+    x, _, gain = _inputs(1003, K, torch.bfloat16, False, seed=K + 1)
+    _check(x, _call(x.to(DEV), None, gain.to(DEV), 1e-5, form), _want(x, None, gain, 1e-5, form), form)
