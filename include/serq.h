@@ -376,7 +376,8 @@ int serq_g128_linear(const void* Xq, const float* scale, const int32_t* zero, in
  * A row whose sum holds an infinity (finite X and residual can add up to one) or NaN: h as it is, scale_out NaN, its codes and zero point undefined; MXFP4
  * with an infinity: rstd = 0, so the other channels' codes are 0 (and their blocks' exponents 127), those of infinite channels undefined; with NaN: undefined.
  * Other rows are not touched by it.
- * The sums of squares are exact enough for every output to be the same whatever the row's split (a sum of fp32 squares rounds in 64 bits).
+ * The root is good to some 2^-50 before it is rounded to fp32, so outputs are the correctly rounded ones, whatever the row's split, but where it lies that close to
+ * a border between two fp32 numbers.
  * M up to 2^30.  Everything else as the quantisers named.
  */
 int serq_rmsnorm_quantize_act(const void* X, const void* residual, int x_dtype, const float* gain, float eps, int64_t M, int64_t K,

@@ -133,6 +133,7 @@ size_t serq_paged_attn_workspace_bytes(int64_t tokens, int seqs, int max_q, int6
  * (their page numbers are clamped); pages outside are not.  With a cap a product of -inf has the score -cap and weighs as such.  A capped score is good to
  * cap * 2^-20 beside what scale * q.K_j is; a biased one is an fp32 sum that the bias is part of, so it is good to about
  * 2^-24 (dim + 8) slopes[h] |p - j| (of no account where a row sees keys near its own; a row whose nearest key has a bias beyond 2^24 may count as one that sees none).
+ * Chunks over a long cache are cut into slices by max_kv, not by what their rows see: where that is little of it, few of the slices have work.
  * Everything else (workspace, bounds, types) as serq_paged_attn.
  */
 #define SERQ_ATTN_MAX_CAP 1024.0f

@@ -4,8 +4,8 @@
 // Few rows are bound by memory with or without them: 40 tokens over up to 8000 keys 85 us plain, 88 capped; one over 65000, 16 heads of 64 channels, 51 plain, 52
 // with a bias.  Many rows, 32 query and 8 key heads of 128 channels, a prompt of 8192 tokens: plain 484, with a bias 548 (two instructions a score before the products),
 // capped 603 (four a score, two of them an exponential and a reciprocal, between the products with V; E4M3 636, 64 channels 436); with a prefix
-// of 5531 of them seen both ways 710 for 1.46 times the work.  12000 tokens of packed documents, 8.5 tiles a row block: 158, of which what a block begins and
-// ends with is more than half.
+// of 5531 of them seen both ways 710 for 1.46 times the work.  12000 tokens of packed documents, 8.5 tiles a row block: 158 to 166, of which row blocks without
+// a key (their beginnings and ends, q read and the result stored) take 47.
 #pragma once
 
 #include "paged_attn_few.h"

@@ -3,8 +3,8 @@
 // Integer codes are those of u: the norm's factor is one number a token, which symmetric and asymmetric scales carry along
 // (scale = su rstd), so the sum of squares and the largest |u| are found in one round of the workgroup and no code waits
 // for the square root.  MXFP4's block scales are powers of two: there v = u rstd is what is quantised.
-// The sum of squares is taken in 64 bits: squares of 16-bit numbers are exact there and sums of them as good as, so rstd is the correctly rounded
-// one however the row is split, and with it every code and scale is defined to the bit.
+// The sum of squares is taken in 64 bits: squares of 16-bit numbers are exact there and sums of them as good as, so rstd is good to some 2^-50 before its one
+// rounding to fp32 however the row is split: the correctly rounded one but where that lies as close to a border, and with it every code and scale.
 //
 // A workgroup a token, the row in registers between the two steps.  Bound by memory: stream, residual and sum in 16 bits and 8-bit codes are 7 bytes
 // a channel, 16384 tokens of 4096 channels 470 MB in 81.2 us (5.8 TB/s; a copy of 1 GiB reaches 5.1 to 5.3); few tokens by the trip to
